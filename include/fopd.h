@@ -70,6 +70,7 @@ typedef enum {
   FOPD_EHIP = 9,         /* a HIP runtime call or kernel launch failed */
   FOPD_ESETS = 10,       /* device flag: mask bytes 2 / 3 (the two aligned sets differ) in a chunk call made without n_roll_in */
   FOPD_ELIMIT = 11,      /* T or B beyond the fixed limits of an entry point that owns its scratch memory */
+  FOPD_EDIST = 12,       /* device flag: a row of logits that is no distribution, a negative temperature, variates that are no numbers */
   FOPD_STATUS_ANY_INT = 0x7fffffff   /* not a status: makes every int a value of the type, so that a caller's
                                         out-of-range code reaches fopd_status_string's default branch defined */
 } fopd_status;
@@ -99,8 +100,8 @@ size_t fopd_workspace_bytes(int64_t T, int32_t B);
 fopd_status fopd_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
 
 /* HOST-SYNCHRONOUS.  Waits for `stream`, reads the sticky device flags and returns FOPD_OK or the
- * first of FOPD_ETOKEN_RANGE, FOPD_ESEGMENTS, FOPD_ELAG, FOPD_ESETS that is set.  If flags_host is not
- * NULL it receives the raw bit mask (bit 0 token range, bit 1 segments, bit 2 lag, bit 3 aligned sets). */
+ * first of FOPD_ETOKEN_RANGE, FOPD_ESEGMENTS, FOPD_ELAG, FOPD_ESETS, FOPD_EDIST that is set.  If flags_host is not
+ * NULL it receives the raw bit mask (bit 0 token range, bit 1 segments, bit 2 lag, bit 3 aligned sets, bit 4 no distribution). */
 fopd_status fopd_workspace_status(const void* workspace, void* stream, int32_t* flags_host);
 
 /* HOST ONLY.  The status that a raw flag word (as above) stands for. */
@@ -594,6 +595,117 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
     int64_t rows_chunk, float* loss, float* freshness, float* weights, float* logp, float* lse, float* token_loss,
     float* dhidden, int64_t lddh, float* dweight, int64_t lddw, int accumulate_dweight, void* workspace,
     size_t workspace_bytes, void* stream);
+
+/*
+ * Matrices in microscaled 4-bit floating point, and the output projection kept in it.
+ *
+ * 32 neighbouring entries of a row share a power of two: x_k is held as 2^s e_k with e_k one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * its sign (E2M1), s = max(floor(log2 max|x|) - 2, -127) (E8M0).  Entries are rounded to nearest, ties to even, and entries past
+ * 6 2^s to 6 2^s (MX 1.0's rule for the scale puts the largest one at 4 .. 7.99).  A block that holds an infinity or a NaN is
+ * held as 32 NaN.  d need not be a multiple of 32: the last block is shorter.
+ *
+ * A packed matrix is one buffer of fopd_mx4_bytes(R, d) bytes, 16-byte aligned, written whole by fopd_mx4_quantize:
+ *   codes   row by row, ceil(d / 256) x 128 bytes a row, entry k in half k % 2 (0: the low one) of byte k / 2, zeros behind
+ *           entry d - 1; then up to the next multiple of 256 bytes nothing
+ *   scales  s + 127 of block b (32 entries) of row r at byte ((r / 64) ceil(d / 256) + b / 8) 512 +
+ *           8 (16 (b % 4) + r % 16) + 2 (r / 16 % 4) + b / 4 % 2 behind that; 255 marks a block of NaN
+ *
+ * fopd_mx4_quantize    in [R, ld] of `dt` -> packed; columns d .. ld - 1 are not read
+ * fopd_mx4_dequantize  packed -> out [R, ldo] of `dt`; every value that a block of bf16 entries gives is exact in bf16
+ * fopd_mx4_logits      logits[t, v] = sum_k hidden[t, k] weight[v, k], both in 4-bit blocks: hidden [T, ldh] of `dt_hidden`
+ *                      is quantised on the way (into the workspace), `weight` is the packed [V, d] projection, laid out
+ *                      once.  fp32 sums, rounded once to `dt`; columns V .. ld - 1 of the logits are not written.  What a
+ *                      drafter runs for each token it proposes (fopd_verify_draft takes its logits), or a scoring pass
+ *                      whose teacher or policy is served with such a projection.
+ *   workspace          fopd_mx4_logits_workspace_bytes(T, V, d) bytes, 256-byte aligned; nothing in it has to be initialised
+ * The sum over k of a result is taken in an order that goes by T, V and d, not by its place: the same hidden row in a call of
+ * another T may differ in its last bits.  The first call in a process sets a kernel attribute: make one call before
+ * capturing fopd_mx4_logits into a HIP graph.  T = 0 or R = 0 does nothing.
+ */
+size_t fopd_mx4_bytes(int64_t R, int64_t d);
+fopd_status fopd_mx4_quantize(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed,
+                              size_t packed_bytes, void* stream);
+fopd_status fopd_mx4_dequantize(const void* packed, size_t packed_bytes, int64_t R, int64_t d, void* out, fopd_dtype dt,
+                                int64_t ldo, void* stream);
+size_t fopd_mx4_logits_workspace_bytes(int64_t T, int64_t V, int64_t d);
+fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ldh, const void* weight, size_t weight_bytes,
+                            int64_t T, int64_t V, int64_t d, void* logits, fopd_dtype dt, int64_t ld, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens: rollouts in which a cheap drafter proposes the next tokens and the student, which has run
+ * over all of them at once, keeps those that leave its own distribution unchanged, and adds one.  The tokens that come out
+ * are samples of the student, and their log-probabilities are the behaviour log-probabilities that the loss takes.
+ *
+ * Sample i has draft_lens[i] = n drafted tokens and n + 1 rows, row j (j = 0 .. n) of the sample in row row_begin[i] + j of
+ * every per-row array: target_logits row j is the student's distribution p_j of the token at place j, draft_logits row j the
+ * drafter's q_j, from which draft_ids[j] was drawn, accept_u[j] a uniform variate of [0, 1).  Draft j is kept while
+ *     accept_u[j] q_j(draft_ids[j]) < p_j(draft_ids[j]),
+ * p_j = softmax(target row / tau_i), q_j = softmax(draft row / tau_i); a = n_accepted[i] is the number of tokens before the first one that
+ * is not.  The token at place a is that of the largest r_v / noise[i, v], r_v = max(p_a(v) - q_a(v), 0) if a < n, else p_a(v);
+ * noise are exponential variates, so it is distributed as r made to add up to 1.  (r = 0 everywhere, possible only by
+ * rounding: p_a.)  Ties go to the lowest index.  tau_i = 0 is greedy decoding: draft j is kept while it is the first largest
+ * entry of its row, the last token is that of row a; p is then the softmax at tau = 1, and neither variates nor draft_logits
+ * are read.
+ *
+ *   target_logits  [R, ld] of `dt`; rows that no sample names are not read
+ *   draft_logits   [R, ld_draft] of `dt`, row n of a sample is not read; NULL: drafts without a distribution (looked up): q_j is 1 at the
+ *                  drafted token
+ *   draft_ids      [R] int32 (entry n of a sample is not read); may be NULL with max_draft = 0, which draws a token per sample
+ *   row_begin      [B] int64 or NULL: sample i has rows (max_draft + 1) i on (a padded batch; R >= B (max_draft + 1))
+ *   draft_lens     [B] int32, 0 .. max_draft, or NULL: all max_draft
+ *   max_draft      0 .. 1023;  B (max_draft + 1) <= 2^20
+ *   temperature    [B] f32 >= 0 or NULL: 1
+ *   accept_u       [R] f32 (entry n of a sample is not read)        noise  [B, ld_noise] f32, positive, 16-byte aligned,
+ *                  ld_noise >= V a multiple of 4.  Both NULL: all samples greedily
+ *   n_accepted     [B] int32 out
+ *   out_ids, out_logp, out_mask   [R] int32, f32, uint8 out: rows 0 .. a of a sample get the token, log p_j(token) and 1, its
+ *                  rows behind -1, 0 and 0 (up to max_draft in a padded batch): token_ids, behav_logp and mask of the loss.
+ *                  Rows of no sample stay as they were.  Samples must not share rows.
+ *   workspace      fopd_verify_workspace_bytes(R, V, B) bytes, 256-byte aligned, initialised once with fopd_workspace_init
+ *
+ * On the device: draft_lens outside 0 .. max_draft or rows outside [0, R) raise FOPD_ESEGMENTS, n_accepted is 0 and no row is
+ * written (in a padded batch: -1, 0, 0).  A drafted id outside [0, V) raises FOPD_ETOKEN_RANGE and is not kept.  A row that is
+ * reached and is no distribution (no finite entry, NaN, +inf; or tau_i negative, NaN or infinite) raises FOPD_EDIST; the sample ends before it
+ * with id -1, log-prob NaN and mask 0.  Entries of -inf have probability 0.  Rows behind the first token that is not
+ * kept do not matter, whatever is in them.
+ */
+size_t fopd_verify_workspace_bytes(int64_t R, int64_t V, int32_t B);
+fopd_status fopd_verify_draft(const void* target_logits, const void* draft_logits, fopd_dtype dt, int64_t R, int64_t V,
+                              int64_t ld, int64_t ld_draft, const int32_t* draft_ids, const int64_t* row_begin,
+                              const int32_t* draft_lens, int32_t B, int32_t max_draft, const float* temperature,
+                              const float* accept_u, const float* noise, int64_t ld_noise, int32_t* n_accepted,
+                              int32_t* out_ids, float* out_logp, uint8_t* out_mask, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/*
+ * Global norm of a list of gradients and clipping by it, between the loss's gradients and the optimiser
+ * (theta <- theta - eta grad L of Algorithm 1 with a bounded step).
+ *
+ * fopd_grad_norm   sum_sq[0] = sum over all entries of all tensors of grad^2 (64 bits), norm[0] = its root (f32, may be NULL).
+ *                  With accumulate != 0 the sum is added to what sum_sq holds: lists that do not fit one call; with gradients
+ *                  sharded over ranks, sum_sq of the ranks are added up by the caller between the two calls.
+ * fopd_grad_clip   out = c grad,  c = min(1, max_norm / (sqrt(sum_sq[0]) + eps)), rounded to f32; coef[0] = c (may be NULL).  The
+ *                  product is rounded once to out's type.  A tensor clipped in place with c = 1 is left as it is.
+ *                  A norm that is NaN or infinite makes c NaN or 0, and the results accordingly.
+ * A tensor is `rows` rows of `cols` entries, row r at grad + r ld; out likewise with ld_out, of the same shape.  Only the alignment of
+ * the element type is needed (16 bytes are faster).  out == grad (then of the same type and pitch) clips in place; else
+ * no memory may be shared.  rows or cols of 0 are allowed, and so is n = 0 (sum 0).  fopd_grad_norm does not use out.
+ * `tensors_host` is HOST memory, read before the call returns; the pointers in it are device pointers.
+ *   workspace of fopd_grad_norm: fopd_grad_workspace_bytes() bytes, 256-byte aligned; nothing in it has to be initialised
+ */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t rows, cols, ld, ld_out;
+  fopd_dtype dt, dt_out;
+} fopd_grad_tensor;
+
+size_t fopd_grad_workspace_bytes(void);
+fopd_status fopd_grad_norm(const fopd_grad_tensor* tensors_host, int32_t n, int accumulate, double* sum_sq, float* norm,
+                           void* workspace, size_t workspace_bytes, void* stream);
+fopd_status fopd_grad_clip(const fopd_grad_tensor* tensors_host, int32_t n, const double* sum_sq, float max_norm, float eps,
+                           float* coef, void* stream);
 
 /*
  * Per-kernel timing for benchmarks.  While enabled, every launch of the two streaming kernels

@@ -24,6 +24,9 @@ SYMBOLS = (
     "fopd_lm_head_workspace_bytes", "fopd_lm_head_token_logprobs",
     "fopd_lm_head_loss_workspace_bytes", "fopd_lm_head_loss_fwd_bwd",
     "fopd_lm_head_loss_topk_workspace_bytes", "fopd_lm_head_loss_fwd_bwd_topk_teacher",
+    "fopd_mx4_bytes", "fopd_mx4_quantize", "fopd_mx4_dequantize", "fopd_mx4_logits_workspace_bytes", "fopd_mx4_logits",
+    "fopd_verify_workspace_bytes", "fopd_verify_draft",
+    "fopd_grad_workspace_bytes", "fopd_grad_norm", "fopd_grad_clip",
 )
 
 
@@ -138,6 +141,27 @@ def load_library():
     lib.fopd_profile_reset.argtypes = []
     lib.fopd_profile_read.restype = ctypes.c_int
     lib.fopd_profile_read.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
+    lib.fopd_mx4_bytes.restype = sz
+    lib.fopd_mx4_bytes.argtypes = [i64, i64]
+    lib.fopd_mx4_quantize.restype = ctypes.c_int
+    lib.fopd_mx4_quantize.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, sz, vp]
+    lib.fopd_mx4_dequantize.restype = ctypes.c_int
+    lib.fopd_mx4_dequantize.argtypes = [vp, sz, i64, i64, vp, ctypes.c_int, i64, vp]
+    lib.fopd_mx4_logits_workspace_bytes.restype = sz
+    lib.fopd_mx4_logits_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.fopd_mx4_logits.restype = ctypes.c_int
+    lib.fopd_mx4_logits.argtypes = [vp, ctypes.c_int, i64, vp, sz, i64, i64, i64, vp, ctypes.c_int, i64, vp, sz, vp]
+    lib.fopd_verify_workspace_bytes.restype = sz
+    lib.fopd_verify_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.fopd_verify_draft.restype = ctypes.c_int
+    lib.fopd_verify_draft.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, i32, i32, vp, vp, vp, i64,
+                                      vp, vp, vp, vp, vp, sz, vp]
+    lib.fopd_grad_workspace_bytes.restype = sz
+    lib.fopd_grad_workspace_bytes.argtypes = []
+    lib.fopd_grad_norm.restype = ctypes.c_int
+    lib.fopd_grad_norm.argtypes = [vp, i32, ctypes.c_int, vp, vp, vp, sz, vp]
+    lib.fopd_grad_clip.restype = ctypes.c_int
+    lib.fopd_grad_clip.argtypes = [vp, i32, vp, f32, f32, vp, vp]
     _lib = lib
     return lib
 
@@ -542,3 +566,123 @@ def fopd_profile_read(which):
     n = ctypes.c_int64(0)
     _check(load_library().fopd_profile_read(int(which), ctypes.byref(ms), ctypes.byref(n)), "fopd_profile_read")
     return float(ms.value), int(n.value)
+
+
+def fopd_mx4_bytes(R, d):
+    return int(load_library().fopd_mx4_bytes(int(R), int(d)))
+
+
+def fopd_mx4_quantize(x, dt, R, d, ld, packed, stream=None):
+    import torch
+    p, n = _ws(packed)
+    _check(load_library().fopd_mx4_quantize(_ptr(x, (torch.float32, torch.bfloat16), "x"), int(dt), int(R), int(d), int(ld),
+                                            p, n, _stream(stream)), "fopd_mx4_quantize")
+
+
+def fopd_mx4_dequantize(packed, R, d, out, dt, ldo, stream=None):
+    import torch
+    p, n = _ws(packed)
+    _check(load_library().fopd_mx4_dequantize(p, n, int(R), int(d), _ptr(out, (torch.float32, torch.bfloat16), "out"), int(dt),
+                                              int(ldo), _stream(stream)), "fopd_mx4_dequantize")
+
+
+def fopd_mx4_logits_workspace_bytes(T, V, d):
+    return int(load_library().fopd_mx4_logits_workspace_bytes(int(T), int(V), int(d)))
+
+
+def fopd_mx4_logits(hidden, dt_hidden, ldh, weight, T, V, d, logits, dt, ld, workspace, stream=None):
+    """weight: the packed [V, d] projection that fopd_mx4_quantize wrote."""
+    import torch
+    kinds = (torch.float32, torch.bfloat16)
+    wp, wn = _ws(weight)
+    p, n = _ws(workspace)
+    _check(load_library().fopd_mx4_logits(_ptr(hidden, kinds, "hidden"), int(dt_hidden), int(ldh), wp, wn, int(T), int(V),
+                                          int(d), _ptr(logits, kinds, "logits"), int(dt), int(ld), p, n, _stream(stream)),
+           "fopd_mx4_logits")
+
+
+def fopd_verify_workspace_bytes(R, V, B):
+    return int(load_library().fopd_verify_workspace_bytes(int(R), int(V), int(B)))
+
+
+def fopd_verify_draft(target_logits, draft_logits, dt, R, V, ld, ld_draft, draft_ids, row_begin, draft_lens, B, max_draft,
+                      temperature, accept_u, noise, ld_noise, n_accepted, out_ids, out_logp, out_mask, workspace,
+                      stream=None):
+    import torch
+    kinds, f32, i32 = (torch.float32, torch.bfloat16), torch.float32, torch.int32
+    p, n = _ws(workspace)
+    st = load_library().fopd_verify_draft(
+        _ptr(target_logits, kinds, "target_logits"), _ptr(draft_logits, kinds, "draft_logits"), int(dt), int(R), int(V),
+        int(ld), int(ld_draft), _ptr(draft_ids, i32, "draft_ids"), _ptr(row_begin, torch.int64, "row_begin"),
+        _ptr(draft_lens, i32, "draft_lens"), int(B), int(max_draft), _ptr(temperature, f32, "temperature"),
+        _ptr(accept_u, f32, "accept_u"), _ptr(noise, f32, "noise"), int(ld_noise), _ptr(n_accepted, i32, "n_accepted"),
+        _ptr(out_ids, i32, "out_ids"), _ptr(out_logp, f32, "out_logp"), _ptr(out_mask, torch.uint8, "out_mask"), p, n,
+        _stream(stream))
+    _check(st, "fopd_verify_draft")
+
+
+class GradTensor(ctypes.Structure):
+    """fopd_grad_tensor: one gradient of a list and where its scaled copy goes."""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("dt", ctypes.c_int), ("dt_out", ctypes.c_int)]
+
+
+class GradList:
+    """The list that fopd_grad_norm and fopd_grad_clip take: made once for gradients that stay where they are.  It holds the
+    tensors, so that their memory does."""
+
+    def __init__(self, entries, tensors):
+        self.entries, self.tensors, self.n = entries, tensors, len(tensors)
+
+
+def _grad_shape(t, name):
+    """(rows, cols, pitch) of a tensor that is contiguous, or a matrix whose rows are."""
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("%s has dtype %s, expected float32 or bfloat16" % (name, t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must live in device memory" % name)
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t.shape[0], t.shape[1], t.stride(0)
+    raise ValueError("%s must be contiguous, or a matrix with contiguous rows" % name)
+
+
+def grad_tensors(grads, outs=None):
+    """A GradList of device tensors.  outs: where the scaled gradients go, of the same shapes; None: in place."""
+    import torch
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if len(outs) != len(grads):
+        raise ValueError("as many outs as grads")
+    entries = (GradTensor * max(1, len(grads)))()
+    for e, g, o in zip(entries, grads, outs):
+        if g.shape != o.shape:
+            raise ValueError("outs have the shapes of grads")
+        (rows, cols, ld), (rows_o, _, ld_o) = _grad_shape(g, "grads"), _grad_shape(o, "outs")
+        if rows != rows_o:                              # one of them has gaps: row by row on both sides
+            rows, cols = g.shape
+            ld, ld_o = g.stride(0), o.stride(0)
+        e.grad, e.out, e.rows, e.cols, e.ld, e.ld_out = g.data_ptr(), o.data_ptr(), rows, cols, ld, ld_o
+        e.dt, e.dt_out = (FOPD_F32 if t.dtype is torch.float32 else FOPD_BF16 for t in (g, o))
+    return GradList(entries, list(zip(grads, outs)))
+
+
+def fopd_grad_workspace_bytes():
+    return int(load_library().fopd_grad_workspace_bytes())
+
+
+def fopd_grad_norm(tensors, sum_sq, norm, workspace, accumulate=False, stream=None):
+    import torch
+    p, n = _ws(workspace)
+    _check(load_library().fopd_grad_norm(ctypes.cast(tensors.entries, ctypes.c_void_p), tensors.n, int(bool(accumulate)),
+                                         _ptr(sum_sq, torch.float64, "sum_sq"), _ptr(norm, torch.float32, "norm"), p, n,
+                                         _stream(stream)), "fopd_grad_norm")
+
+
+def fopd_grad_clip(tensors, sum_sq, max_norm, eps, coef, stream=None):
+    import torch
+    _check(load_library().fopd_grad_clip(ctypes.cast(tensors.entries, ctypes.c_void_p), tensors.n,
+                                         _ptr(sum_sq, torch.float64, "sum_sq"), float(max_norm), float(eps),
+                                         _ptr(coef, torch.float32, "coef"), _stream(stream)), "fopd_grad_clip")

@@ -14,6 +14,9 @@
 #include "fopd_kernels.hip"
 #include "fopd_lm_head.hip"
 #include "fopd_gemm.hip"
+#include "fopd_grad.hip"
+#include "fopd_mx4.hip"
+#include "fopd_verify.hip"
 
 namespace {
 
@@ -645,6 +648,146 @@ fopd_status loss_fwd_bwd_check_args(const void* logits, fopd_dtype dt, int64_t T
   return FOPD_OK;
 }
 
+
+// ---- 4-bit matrices -----------------------------------------------------------------------
+
+fopd_status check_mx4(const void* packed, size_t bytes, int64_t R, int64_t d) {
+  if (R < 0 || R > 2147483647LL || d <= 0 || d > 2147483647LL - kMxStep) return FOPD_ESHAPE;
+  if (packed == nullptr) return FOPD_EINVAL;
+  if (misaligned(packed, 16)) return FOPD_EALIGN;
+  if (bytes < static_cast<size_t>(Mx4Layout(R, d).total)) return FOPD_EWORKSPACE;
+  return FOPD_OK;
+}
+
+// launch(first group of 64 rows, groups): a workgroup of 256 lanes for each group and step.
+template <typename Launch>
+fopd_status mx4_in_slabs(const Mx4Layout& at, Launch launch) {
+  const int64_t most = std::max<int64_t>(1, (1LL << 22) / at.steps);
+  for (int64_t g = 0; g < at.groups; g += most) {
+    launch(g, static_cast<unsigned>(std::min(at.groups - g, most) * at.steps));
+    const fopd_status st = launched();
+    if (st != FOPD_OK) return st;
+  }
+  return FOPD_OK;
+}
+
+fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed, hipStream_t s) {
+  auto kern = dt == FOPD_BF16 ? fopd_mx4_pack<FOPD_BF16> : fopd_mx4_pack<FOPD_F32>;
+  return mx4_in_slabs(Mx4Layout(R, d), [&](int64_t g, unsigned n) {
+    kern<<<n, kMxThreads, 0, s>>>(in, ld, R, d, static_cast<unsigned char*>(packed), g);
+  });
+}
+
+// weight [V, d] and hidden rows [T, d], both packed.
+fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
+                               fopd_dtype dt, int64_t ldo, hipStream_t s) {
+  const int blocks = T <= 16 ? 1 : (T <= 32 ? 2 : 4);
+  const dim3 grid(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((T + 16 * blocks - 1) / (16 * blocks)));
+  auto kern = dt == FOPD_BF16 ? (blocks == 1 ? fopd_mx4_few<FOPD_BF16, 1> : blocks == 2 ? fopd_mx4_few<FOPD_BF16, 2> : fopd_mx4_few<FOPD_BF16, 4>)
+                              : (blocks == 1 ? fopd_mx4_few<FOPD_F32, 1> : blocks == 2 ? fopd_mx4_few<FOPD_F32, 2> : fopd_mx4_few<FOPD_F32, 4>);
+  kern<<<grid, kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
+  return launched();
+}
+
+// ---- verification of drafted tokens ---------------------------------------------------------
+
+// How a call is cut: pieces of a row in the first kernel (a power of two), pieces of a race.  Both go by sizes that the workspace
+// is asked for with, so neither depends on the type or on the lengths.
+struct VerifyPlan {
+  int splits, pieces;
+  size_t parts, races, verdicts, total;
+  VerifyPlan(int64_t R, int64_t V, int32_t B) {
+    const int64_t rows = R < 1 ? 1 : R, samples = B < 1 ? 1 : B;
+    splits = 1;
+    while (splits < kVerifyMaxSplits && splits * rows < 4096 && V / (2 * splits) >= 2048) splits *= 2;
+    pieces = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((V + 2047) / 2048, 2048 / samples)));
+    size_t off = 256;
+    parts = Workspace::take(off, 2 * static_cast<size_t>(rows) * splits * sizeof(RowPart));
+    races = Workspace::take(off, static_cast<size_t>(samples) * pieces * sizeof(RacePart));
+    verdicts = Workspace::take(off, static_cast<size_t>(samples) * sizeof(Verdict));
+    total = off;
+  }
+};
+
+template <int DT>
+fopd_status launch_verify(const VerifyArgs& a, const VerifyPlan& plan, void* ws, hipStream_t s) {
+  const int nvec = a.V / Elem<DT>::kPerVec;
+  const unsigned units = static_cast<unsigned>(a.B) * static_cast<unsigned>(a.K + 1) * (a.draft != nullptr ? 2u : 1u);
+  int splits = plan.splits;                                // (many places for few rows: a launch has at most 2^32 lanes)
+  while (splits > 1 && static_cast<int64_t>(units) * splits > kLaunchRows * 4) splits /= 2;
+  RowPart* parts = at<RowPart>(ws, plan.parts);
+  RacePart* races = at<RacePart>(ws, plan.races);
+  Verdict* verdicts = at<Verdict>(ws, plan.verdicts);
+  int32_t* flags = at<int32_t>(ws, 0);
+  fopd_verify_rows<DT><<<units * splits, kVerifyThreads, 0, s>>>(a, splits, (nvec + splits - 1) / splits, parts);
+  fopd_verify_race<DT><<<static_cast<unsigned>(a.B) * plan.pieces, kVerifyThreads, 2 * (a.K + 1) * sizeof(RowPart), s>>>(
+      a, splits, parts, plan.pieces, (nvec + plan.pieces - 1) / plan.pieces, races, verdicts, flags);
+  fopd_verify_finish<DT><<<static_cast<unsigned>(a.B), 64, 0, s>>>(a, plan.pieces, races, verdicts, flags);
+  return launched();
+}
+
+// ---- gradient norm and clipping ------------------------------------------------------------
+
+constexpr int kGradPartials = 1 << 16;
+constexpr int kGradGrid = 2048;                           // workgroups of a launch: eight a compute unit
+
+fopd_status check_grad_tensor(const fopd_grad_tensor& t, bool with_out) {
+  if ((t.dt != FOPD_F32 && t.dt != FOPD_BF16) || (with_out && t.dt_out != FOPD_F32 && t.dt_out != FOPD_BF16)) return FOPD_EDTYPE;
+  constexpr int64_t kMost = 1LL << 40;
+  if (t.rows < 0 || t.cols < 0 || t.rows > kMost || t.cols > kMost) return FOPD_ESHAPE;
+  if (t.rows == 0 || t.cols == 0) return FOPD_OK;
+  if (t.rows > 1 && (t.ld < t.cols || (with_out && t.ld_out < t.cols))) return FOPD_ESHAPE;
+  if (t.grad == nullptr || (with_out && t.out == nullptr)) return FOPD_EINVAL;
+  if (with_out && t.out == t.grad && (t.dt != t.dt_out || (t.rows > 1 && t.ld != t.ld_out))) return FOPD_EINVAL;
+  if (misaligned(t.grad, t.dt == FOPD_F32 ? 4 : 2) || (with_out && misaligned(t.out, t.dt_out == FOPD_F32 ? 4 : 2))) return FOPD_EALIGN;
+  return FOPD_OK;
+}
+
+// launch(table) for the tensors of a list, kGradTable of them or kGradMaxPieces pieces at a time.
+template <typename Launch>
+fopd_status grad_tables(const fopd_grad_tensor* tensors, int32_t n, bool with_out, Launch launch) {
+  GradTable g;
+  g.n = g.pieces = 0;
+  auto flush = [&]() {
+    if (g.n == 0) return FOPD_OK;
+    const fopd_status st = launch(g);
+    g.n = g.pieces = 0;
+    return st;
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    const fopd_grad_tensor& t = tensors[i];
+    if (t.rows == 0 || t.cols == 0) continue;
+    int64_t rows = t.rows, cols = t.cols;
+    if (t.ld == t.cols && (!with_out || t.ld_out == t.cols)) {          // no gaps: one row
+      cols *= rows;
+      rows = 1;
+    }
+    const int64_t row_pieces = (cols + kGradPiece - 1) / kGradPiece;
+    if (row_pieces > kGradMaxPieces) return FOPD_ESHAPE;
+    for (int64_t r = 0; r < rows;) {
+      const int64_t here = std::min(rows - r, std::max<int64_t>(1, kGradMaxPieces / row_pieces));
+      if (g.n == kGradTable || g.pieces + here * row_pieces > kGradMaxPieces) {
+        const fopd_status st = flush();
+        if (st != FOPD_OK) return st;
+      }
+      GradEntry& e = g.t[g.n++];
+      e.grad = static_cast<const char*>(t.grad) + r * t.ld * (t.dt == FOPD_BF16 ? 2 : 4);
+      e.out = with_out ? static_cast<char*>(t.out) + r * t.ld_out * (t.dt_out == FOPD_BF16 ? 2 : 4) : nullptr;
+      e.cols = cols;
+      e.ld = t.ld;
+      e.ld_out = t.ld_out;
+      e.rows = static_cast<int32_t>(here);
+      e.row_pieces = static_cast<int32_t>(row_pieces);
+      e.first_piece = g.pieces;
+      e.bf16 = t.dt == FOPD_BF16;
+      e.out_bf16 = t.dt_out == FOPD_BF16;
+      g.pieces += static_cast<int32_t>(here * row_pieces);
+      r += here;
+    }
+  }
+  return flush();
+}
+
 }  // namespace
 
 extern "C" {
@@ -663,6 +806,7 @@ const char* fopd_status_string(fopd_status status) {
     case FOPD_EHIP: return "HIP runtime or launch failure";
     case FOPD_ESETS: return "mask names two different aligned sets but only one count array was given (rows dropped)";
     case FOPD_ELIMIT: return "size beyond the fixed limits of the entry point";
+    case FOPD_EDIST: return "no distribution: a row of logits without a finite entry, a temperature below 0 or variates that are no numbers";
     default: return "unknown status";
   }
 }
@@ -690,6 +834,7 @@ fopd_status fopd_flags_status(int32_t flags) {
   if (flags & kFlagSegments) return FOPD_ESEGMENTS;
   if (flags & kFlagLag) return FOPD_ELAG;
   if (flags & kFlagSets) return FOPD_ESETS;
+  if (flags & kFlagDist) return FOPD_EDIST;
   return FOPD_OK;
 }
 
@@ -1776,6 +1921,141 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
                            B, hp, freshness_in, n_train_in, n_roll_in, seq_lens_host, grad_scale, rows_chunk, loss, freshness,
                            weights, logp, lse, dhidden, lddh, dweight, lddw, accumulate_dweight, &listed, workspace,
                            workspace_bytes, stream);
+}
+
+size_t fopd_mx4_bytes(int64_t R, int64_t d) {
+  return static_cast<size_t>(Mx4Layout(R < 0 ? 0 : R, d < 0 ? 0 : d).total);
+}
+
+fopd_status fopd_mx4_quantize(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed,
+                              size_t packed_bytes, void* stream) {
+  fopd_status st = check_matrix(in, dt, R, d, ld);
+  if (st != FOPD_OK) return st;
+  st = check_mx4(packed, packed_bytes, R, d);
+  if (st != FOPD_OK || R == 0) return st;
+  return launch_mx4_pack(in, dt, R, d, ld, packed, static_cast<hipStream_t>(stream));
+}
+
+fopd_status fopd_mx4_dequantize(const void* packed, size_t packed_bytes, int64_t R, int64_t d, void* out, fopd_dtype dt,
+                                int64_t ldo, void* stream) {
+  fopd_status st = check_matrix(out, dt, R, d, ldo);
+  if (st != FOPD_OK) return st;
+  st = check_mx4(packed, packed_bytes, R, d);
+  if (st != FOPD_OK || R == 0) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto kern = dt == FOPD_BF16 ? fopd_mx4_unpack<FOPD_BF16> : fopd_mx4_unpack<FOPD_F32>;
+  return mx4_in_slabs(Mx4Layout(R, d), [&](int64_t g, unsigned n) {
+    kern<<<n, kMxThreads, 0, s>>>(static_cast<const unsigned char*>(packed), R, d, out, ldo, g);
+  });
+}
+
+size_t fopd_mx4_logits_workspace_bytes(int64_t T, int64_t V, int64_t d) {
+  (void)V;
+  return 256 + align_up(fopd_mx4_bytes(T, d), 256);
+}
+
+fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ldh, const void* weight, size_t weight_bytes,
+                            int64_t T, int64_t V, int64_t d, void* logits, fopd_dtype dt, int64_t ld, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  fopd_status st = check_matrix(hidden, dt_hidden, T, d, ldh);
+  if (st != FOPD_OK) return st;
+  st = check_matrix(logits, dt, T, V, ld);
+  if (st != FOPD_OK) return st;
+  st = check_mx4(weight, weight_bytes, V, d);
+  if (st != FOPD_OK) return st;
+  if (workspace == nullptr || misaligned(workspace, 256) || workspace_bytes < fopd_mx4_logits_workspace_bytes(T, V, d))
+    return FOPD_EWORKSPACE;
+  if (T == 0) return FOPD_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  unsigned char* packed = at<unsigned char>(workspace, 256);
+  st = launch_mx4_pack(hidden, dt_hidden, T, d, ldh, packed, s);
+  if (st != FOPD_OK) return st;
+  return launch_mx4_product(static_cast<const unsigned char*>(weight), V, packed, T, d, logits, dt, ld, s);
+}
+
+size_t fopd_verify_workspace_bytes(int64_t R, int64_t V, int32_t B) { return VerifyPlan(R, V, B).total; }
+
+fopd_status fopd_verify_draft(const void* target_logits, const void* draft_logits, fopd_dtype dt, int64_t R, int64_t V,
+                              int64_t ld, int64_t ld_draft, const int32_t* draft_ids, const int64_t* row_begin,
+                              const int32_t* draft_lens, int32_t B, int32_t max_draft, const float* temperature,
+                              const float* accept_u, const float* noise, int64_t ld_noise, int32_t* n_accepted,
+                              int32_t* out_ids, float* out_logp, uint8_t* out_mask, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  fopd_status st = check_matrix(target_logits, dt, R, V, ld);
+  if (st != FOPD_OK) return st;
+  if (draft_logits != nullptr) {
+    st = check_matrix(draft_logits, dt, R, V, ld_draft);
+    if (st != FOPD_OK) return st;
+  }
+  if (R < 1 || B <= 0 || max_draft < 0 || max_draft > kVerifyMaxDraft || static_cast<int64_t>(B) * (max_draft + 1) > (1 << 20))
+    return FOPD_ESHAPE;
+  if (row_begin == nullptr && R < static_cast<int64_t>(B) * (max_draft + 1)) return FOPD_ESHAPE;
+  if (n_accepted == nullptr || out_ids == nullptr || out_logp == nullptr || out_mask == nullptr) return FOPD_EINVAL;
+  const bool greedy = noise == nullptr;
+  if (max_draft > 0 && (draft_ids == nullptr || greedy != (accept_u == nullptr))) return FOPD_EINVAL;
+  if (!greedy && ld_noise < V) return FOPD_ESHAPE;
+  if (!greedy && (misaligned(noise, 16) || ld_noise % 4 != 0)) return FOPD_EALIGN;
+  const VerifyPlan plan(R, V, B);
+  if (workspace == nullptr || misaligned(workspace, 256) || workspace_bytes < plan.total) return FOPD_EWORKSPACE;
+  const VerifyArgs a = {target_logits, greedy ? nullptr : draft_logits, ld, ld_draft, R, ld_noise, static_cast<int>(V), B, max_draft,
+                        draft_ids, row_begin, draft_lens, temperature, accept_u, noise, n_accepted, out_ids, out_logp, out_mask};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return dt == FOPD_BF16 ? launch_verify<FOPD_BF16>(a, plan, workspace, s) : launch_verify<FOPD_F32>(a, plan, workspace, s);
+}
+
+size_t fopd_grad_workspace_bytes(void) { return 256 + kGradPartials * sizeof(double); }
+
+fopd_status fopd_grad_norm(const fopd_grad_tensor* tensors_host, int32_t n, int accumulate, double* sum_sq, float* norm,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (n < 0) return FOPD_ESHAPE;
+  if ((n > 0 && tensors_host == nullptr) || sum_sq == nullptr) return FOPD_EINVAL;
+  if (workspace == nullptr || misaligned(workspace, 256) || workspace_bytes < fopd_grad_workspace_bytes()) return FOPD_EWORKSPACE;
+  for (int32_t i = 0; i < n; ++i) {
+    const fopd_status st = check_grad_tensor(tensors_host[i], false);
+    if (st != FOPD_OK) return st;
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  double* partial = at<double>(workspace, 256);
+  int used = 0;
+  bool add = accumulate != 0;
+  auto finish = [&](float* to) {
+    fopd_grad_norm_final<<<1, kGradLanes, 0, s>>>(partial, used, add, sum_sq, to);
+    used = 0;
+    add = true;
+    return launched();
+  };
+  const fopd_status st = grad_tables(tensors_host, n, false, [&](const GradTable& g) {
+    const int grid = std::min(g.pieces, kGradGrid);
+    if (used + grid > kGradPartials) {
+      const fopd_status full = finish(nullptr);
+      if (full != FOPD_OK) return full;
+    }
+    fopd_grad_sum_squares<<<static_cast<unsigned>(grid), kGradLanes, 0, s>>>(g, partial + used);
+    used += grid;
+    return launched();
+  });
+  return st != FOPD_OK ? st : finish(norm);
+}
+
+fopd_status fopd_grad_clip(const fopd_grad_tensor* tensors_host, int32_t n, const double* sum_sq, float max_norm, float eps,
+                           float* coef, void* stream) {
+  if (n < 0) return FOPD_ESHAPE;
+  if ((n > 0 && tensors_host == nullptr) || sum_sq == nullptr || !(max_norm >= 0.f) || !(eps >= 0.f)) return FOPD_EINVAL;
+  for (int32_t i = 0; i < n; ++i) {
+    const fopd_status st = check_grad_tensor(tensors_host[i], true);
+    if (st != FOPD_OK) return st;
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto scale = [&](const GradTable& g, int grid) {
+    fopd_grad_scale<<<static_cast<unsigned>(grid), kGradLanes, 0, s>>>(g, sum_sq, max_norm, eps, coef);
+    coef = nullptr;                                        // (written by the first launch)
+    return launched();
+  };
+  const fopd_status st = grad_tables(tensors_host, n, true, [&](const GradTable& g) { return scale(g, std::min(g.pieces, kGradGrid)); });
+  if (st != FOPD_OK || coef == nullptr) return st;
+  GradTable none;
+  none.n = none.pieces = 0;
+  return scale(none, 1);
 }
 
 fopd_status fopd_set_option(const char* name, int value) {

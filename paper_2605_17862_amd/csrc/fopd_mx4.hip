@@ -1,0 +1,278 @@
+// Matrices in microscaled 4-bit floating point, and their product on the matrix cores of gfx950 (CDNA4).
+//
+//   fopd_mx4_pack       rows of fp32 / bf16 into blocks of 32 entries that share a power of two
+//   fopd_mx4_unpack     the values of a packed matrix
+//   fopd_mx4_few        Out[t, v] = sum_k H[t, k] W[v, k] for few rows of H: the weight streamed past them once
+//   fopd_mx4_tiles      the same for many rows, in 256 x 256 tiles
+//
+// A block holds x_k ~ 2^(s - 127) e_k with e_k one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and its sign: s is the exponent of the block's
+// largest magnitude less 2, which puts that entry at 4 .. 7.99; entries are rounded to nearest, ties to even, those past 6 to 6.
+// A block with an infinity or a NaN has s = 255, and all its values are NaN.
+//
+// A packed matrix of R rows of d entries (Mx4Layout):
+//   codes    row by row, two entries a byte, the first in the low half; a row is padded with zeros to whole steps of 256
+//            entries = 128 bytes, which is a half tile's row of one step of the loop in fopd_lm_head.hip
+//   scales   for 64 rows and a step 512 bytes: byte 8 (16 q + row % 16) + 2 (row / 16 % 4) + h is that of the row's block
+//            4 h + q of the step.  In v_mfma_scale_f32_16x16x128_f8f6f4 lane 16 q + r holds row r, entries 32 q .. + 31 of 128, so the
+//            8 bytes of a lane are the scales of its four fragments of 64 rows in both halves of the step: one LDS read of 8
+//            bytes where bytes in the order of the matrix would take 8 reads and a shift each.
+
+#ifndef FOPD_MX4_HIP_
+#define FOPD_MX4_HIP_
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "fopd_kernels.hip"
+#include "fopd_lm_head.hip"
+#include "fopd_gemm.hip"
+
+namespace fopd {
+
+constexpr int kMxStep = 256;                  // entries of a step
+constexpr int kMxRowBytes = 128;              // code bytes of a row and step
+constexpr int kMxScaleBytes = 512;            // scale bytes of 64 rows and a step
+constexpr int kMxThreads = 256;
+
+struct Mx4Layout {
+  int64_t rows, steps, groups, codes, total;  // groups of 64 rows; bytes of the codes (the scales start there) and of all
+  __host__ __device__ Mx4Layout(int64_t R, int64_t d)
+      : rows(R), steps((d + kMxStep - 1) / kMxStep), groups((R + 63) / 64),
+        codes((R * steps * kMxRowBytes + 255) / 256 * 256), total(codes + groups * steps * kMxScaleBytes) {}
+};
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+namespace {
+
+// Place of the scale of block `block` (of the row) in the 512 bytes of its 64 rows and step.
+__host__ __device__ __forceinline__ int mx_scale_at(int row, int block) {
+  return 8 * (16 * (block & 3) + (row & 15)) + 2 * ((row >> 4) & 3) + ((block >> 2) & 1);
+}
+
+// acc += A B over 128 entries; the scales are bytes SA of sa and SB of sb.
+template <int SA, int SB>
+__device__ __forceinline__ f32x4 mx_multiply(const i32x4& a, const i32x4& b, const f32x4& acc, int sa, int sb) {
+  const i32x8 a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+  const i32x8 b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, acc, 4, 4, SA, sa, SB, sb);
+}
+
+// (the bytes are constants of the instruction; in an unrolled loop one case remains)
+__device__ __forceinline__ f32x4 mx_multiply(const i32x4& a, const i32x4& b, const f32x4& acc, int sa, int byte_a, int sb, int byte_b) {
+  switch (byte_a * 4 + byte_b) {
+    case 0: return mx_multiply<0, 0>(a, b, acc, sa, sb);
+    case 1: return mx_multiply<0, 1>(a, b, acc, sa, sb);
+    case 2: return mx_multiply<0, 2>(a, b, acc, sa, sb);
+    case 3: return mx_multiply<0, 3>(a, b, acc, sa, sb);
+    case 4: return mx_multiply<1, 0>(a, b, acc, sa, sb);
+    case 5: return mx_multiply<1, 1>(a, b, acc, sa, sb);
+    case 6: return mx_multiply<1, 2>(a, b, acc, sa, sb);
+    case 7: return mx_multiply<1, 3>(a, b, acc, sa, sb);
+    case 8: return mx_multiply<2, 0>(a, b, acc, sa, sb);
+    case 9: return mx_multiply<2, 1>(a, b, acc, sa, sb);
+    case 10: return mx_multiply<2, 2>(a, b, acc, sa, sb);
+    case 11: return mx_multiply<2, 3>(a, b, acc, sa, sb);
+    case 12: return mx_multiply<3, 0>(a, b, acc, sa, sb);
+    case 13: return mx_multiply<3, 1>(a, b, acc, sa, sb);
+    case 14: return mx_multiply<3, 2>(a, b, acc, sa, sb);
+    default: return mx_multiply<3, 3>(a, b, acc, sa, sb);
+  }
+}
+
+}  // namespace
+
+// Workgroup (group - first_group) x steps + step: 64 rows of one step, sixteen a wavefront.  A block is 32 / E neighbouring lanes of E entries.
+// Columns d and on are zeros and are not read; rows past the last leave scales of 0 behind.
+template <int DT>
+__global__ void __launch_bounds__(kMxThreads)
+fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, unsigned char* __restrict__ packed, int64_t first_group) {
+  constexpr int E = Elem<DT>::kPerVec, kLanesPerRow = kMxStep / E, kRows = 64 / kLanesPerRow;   // rows of a wavefront at a time
+  const Mx4Layout at(R, d);
+  const unsigned steps = static_cast<unsigned>(at.steps), in_launch = blockIdx.x / steps;
+  const int64_t group = first_group + in_launch;
+  const int step = static_cast<int>(blockIdx.x - in_launch * steps);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int part = lane % kLanesPerRow;                    // of a row's step
+  const int64_t col = static_cast<int64_t>(step) * kMxStep + part * E;
+  __shared__ __align__(16) unsigned char scales[kMxScaleBytes];
+  const int row0 = wave * 16 + lane / kLanesPerRow;
+  u32x4 q[16 / kRows];
+#pragma unroll
+  for (int u = 0; u < 16 / kRows; ++u) {
+    const int64_t r = group * 64 + row0 + u * kRows;
+    q[u] = u32x4{0u, 0u, 0u, 0u};
+    if (r >= R || col >= d) continue;
+    const char* p = static_cast<const char*>(in) + (r * ld + col) * Elem<DT>::kBytes;
+    if (col + E <= d) {
+      q[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    } else {
+      float x[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = col + e < d ? load_elem<DT>(p, e) : 0.f;
+      q[u] = pack<DT>(x);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 16 / kRows; ++u) {
+    const int in_group = row0 + u * kRows;
+    const int64_t r = group * 64 + in_group;
+    float x[E];
+    unpack<DT>(q[u], x);
+    uint32_t top = 0;                                      // magnitudes order as their bits do, infinities and NaN above the rest
+#pragma unroll
+    for (int e = 0; e < E; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int off = 1; off < 32 / E; off <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
+    const int exponent = static_cast<int>(top >> 23);
+    const int scale = exponent == 255 ? 255 : max(exponent - 2, 0);
+    // 2^(127 - scale): a power of two, so the product is exact wherever it is not rounded to zero anyway
+    const float inv = exponent == 255 ? 0.f : __uint_as_float(static_cast<uint32_t>(254 - scale) << 23);
+    uint32_t codes = 0;
+    if constexpr (E == 8) {
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0] * inv, x[1] * inv, 1.f, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * inv, x[3] * inv, 1.f, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4] * inv, x[5] * inv, 1.f, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6] * inv, x[7] * inv, 1.f, 3);
+    } else {
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0] * inv, x[1] * inv, 1.f, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * inv, x[3] * inv, 1.f, 1);
+    }
+    if (exponent == 255) codes = 0;
+    if (r < R) {
+      unsigned char* row = packed + (r * at.steps + step) * kMxRowBytes;
+      if constexpr (E == 8) reinterpret_cast<uint32_t*>(row)[part] = codes;
+      else reinterpret_cast<uint16_t*>(row)[part] = static_cast<uint16_t>(codes);
+    }
+    if (part % (32 / E) == 0) scales[mx_scale_at(in_group, part / (32 / E))] = static_cast<unsigned char>(scale);
+  }
+  __syncthreads();
+  if (tid < kMxScaleBytes / 16)
+    reinterpret_cast<u32x4*>(packed + at.codes + (group * at.steps + step) * kMxScaleBytes)[tid] = reinterpret_cast<const u32x4*>(scales)[tid];
+}
+
+// Workgroup (group - first_group) x steps + step, eight entries a lane.
+template <int DT>
+__global__ void __launch_bounds__(kMxThreads)
+fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, void* __restrict__ out, int64_t ldo,
+                int64_t first_group) {
+  typedef float f32x2v __attribute__((ext_vector_type(2)));
+  const Mx4Layout at(R, d);
+  const unsigned steps = static_cast<unsigned>(at.steps), in_launch = blockIdx.x / steps;
+  const int64_t group = first_group + in_launch;
+  const int step = static_cast<int>(blockIdx.x - in_launch * steps);
+  const int tid = threadIdx.x, part = tid & 31;
+  const int64_t col = static_cast<int64_t>(step) * kMxStep + part * 8;
+  __shared__ __align__(16) unsigned char scales[kMxScaleBytes];
+  if (tid < kMxScaleBytes / 16)
+    reinterpret_cast<u32x4*>(scales)[tid] = reinterpret_cast<const u32x4*>(packed + at.codes + (group * at.steps + step) * kMxScaleBytes)[tid];
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int in_group = (tid >> 5) + 8 * u;
+    const int64_t r = group * 64 + in_group;
+    if (r >= R || col >= d) continue;
+    const uint32_t codes = reinterpret_cast<const uint32_t*>(packed + (r * at.steps + step) * kMxRowBytes)[part];
+    const int scale = scales[mx_scale_at(in_group, part >> 2)];
+    const float unit = scale == 255 ? __builtin_nanf("") : __uint_as_float(scale == 0 ? 0x00400000u : static_cast<uint32_t>(scale) << 23);
+    const f32x2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 1);
+    const f32x2v p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 3);
+    const float x[8] = {p0.x * unit, p0.y * unit, p1.x * unit, p1.y * unit, p2.x * unit, p2.y * unit, p3.x * unit, p3.y * unit};
+    char* o = static_cast<char*>(out) + (r * ldo + col) * Elem<DT>::kBytes;
+    if (col + 8 <= d) {
+      u32x4* ov = reinterpret_cast<u32x4*>(o);
+      if constexpr (DT == FOPD_BF16) {
+        __builtin_nontemporal_store(pack<FOPD_BF16>(x), ov);
+      } else {
+        __builtin_nontemporal_store(pack<FOPD_F32>(x), ov);
+        __builtin_nontemporal_store(pack<FOPD_F32>(x + 4), ov + 1);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < d) store_elem<DT>(o, e, x[e]);
+    }
+  }
+}
+
+// Few rows of H: workgroup (x, y) has vocabulary rows 64 x .. + 63 and rows 16 BLOCKS y .. of H.  Its wavefronts take the steps in
+// turn and their sums are added in the LDS; the weight goes from memory to the registers of the one wavefront that needs it.
+template <int DT, int BLOCKS>
+__global__ void __launch_bounds__(kMxThreads)
+fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
+             void* __restrict__ out, int64_t ldo) {
+  constexpr int kWaves = kMxThreads / 64;
+  __shared__ __align__(16) float sums[kWaves][16 * BLOCKS][64 + 4];
+  const Mx4Layout w_at(V, d), h_at(T, d);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int steps = static_cast<int>(w_at.steps);
+  const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64, t0 = static_cast<int64_t>(blockIdx.y) * (16 * BLOCKS);
+  const int64_t row_bytes = w_at.steps * kMxRowBytes;
+  const unsigned char* w[4];
+  const unsigned char* h[BLOCKS];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = W + std::min<int64_t>(v0 + 16 * i + (lane & 15), V - 1) * row_bytes + (lane >> 4) * 16;
+#pragma unroll
+  for (int j = 0; j < BLOCKS; ++j) h[j] = H + std::min<int64_t>(t0 + 16 * j + (lane & 15), T - 1) * row_bytes + (lane >> 4) * 16;
+  const unsigned char* ws = W + w_at.codes + (v0 >> 6) * w_at.steps * kMxScaleBytes + lane * 8;
+  const unsigned char* hs = H + h_at.codes + (t0 >> 6) * h_at.steps * kMxScaleBytes + lane * 8;
+  const int first_block = static_cast<int>((t0 >> 4) & 3);  // of H's 64 rows
+  f32x4 acc[4][BLOCKS];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = wave; s < steps; s += kWaves) {
+    i32x4 a[4][2], b[BLOCKS][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) a[i][ks] = *reinterpret_cast<const i32x4*>(w[i] + s * kMxRowBytes + ks * 64);
+    const uint2 sa = *reinterpret_cast<const uint2*>(ws + static_cast<int64_t>(s) * kMxScaleBytes);
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) b[j][ks] = *reinterpret_cast<const i32x4*>(h[j] + s * kMxRowBytes + ks * 64);
+    uint64_t sb = *reinterpret_cast<const uint64_t*>(hs + static_cast<int64_t>(s) * kMxScaleBytes);
+    sb >>= 16 * first_block;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < BLOCKS; ++j)
+          acc[i][j] = mx_multiply(a[i][ks], b[j][ks], acc[i][j], static_cast<int>(i < 2 ? sa.x : sa.y), 2 * (i & 1) + ks,
+                                  static_cast<int>(j < 2 ? sb : sb >> 32), 2 * (j & 1) + ks);
+  }
+  // register r of acc[i][j]: vocabulary row 16 i + 4 (lane / 16) + r, row 16 j + lane % 16 of H
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j)
+      *reinterpret_cast<f32x4*>(&sums[wave][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4)]) = acc[i][j];
+  __syncthreads();
+  for (int k = tid; k < 16 * BLOCKS * 16; k += kMxThreads) {            // four neighbouring results each
+    const int t = k >> 4, v = 4 * (k & 15);
+    f32x4 z = *reinterpret_cast<const f32x4*>(&sums[0][t][v]);
+#pragma unroll
+    for (int u = 1; u < kWaves; ++u) z += *reinterpret_cast<const f32x4*>(&sums[u][t][v]);
+    if (t0 + t >= T || v0 + v >= V) continue;
+    char* o = static_cast<char*>(out) + ((t0 + t) * ldo + v0 + v) * Elem<DT>::kBytes;
+    if (v0 + v + 4 <= V) {
+      if constexpr (DT == FOPD_BF16) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
+      else *reinterpret_cast<f32x4*>(o) = z;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v0 + v + e < V) store_elem<DT>(o, e, z[e]);
+    }
+  }
+}
+
+}  // namespace fopd
+
+#endif  // FOPD_MX4_HIP_

@@ -1,0 +1,180 @@
+"""4-bit blocks and the projection kept in them, against the float64 oracle."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as oo
+from paper_2605_17862_amd import binding as fb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+KINDS = {"f32": (torch.float32, fb.FOPD_F32, 4), "bf16": (torch.bfloat16, fb.FOPD_BF16, 8)}
+
+
+def _matrix(R, d, kind, seed, spread=8, pitch=None):
+    """Rows of different size, zeros and small entries among them, in a padded buffer whose padding is NaN."""
+    dtype, _, per = KINDS[kind]
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(R, d, generator=g) * torch.exp2(torch.randint(-spread, spread + 1, (R, 1), generator=g).float())
+    x[torch.rand(R, d, generator=g) < 0.1] *= 2.0 ** -6
+    x[torch.rand(R, d, generator=g) < 0.05] = 0.0
+    ld = pitch or (d + per - 1) // per * per
+    buf = torch.full((R, ld), float("nan"), dtype=dtype, device=DEV)
+    buf[:, :d] = x.to(dtype).to(DEV)
+    return buf, buf[:, :d].double().cpu().numpy()
+
+
+def _pack(buf, kind, R, d):
+    packed = torch.zeros(fb.fopd_mx4_bytes(R, d), dtype=torch.uint8, device=DEV)
+    fb.fopd_mx4_quantize(buf, KINDS[kind][1], R, d, buf.shape[1], packed)
+    return packed
+
+
+def _workspace(n):
+    ws = torch.empty(n + 256, dtype=torch.uint8, device=DEV)
+    off = (-ws.data_ptr()) % 256
+    return ws[off:off + n]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("R,d,pitch", [(1, 1, None), (1, 32, None), (3, 31, None), (5, 33, 64), (64, 256, None), (65, 257, 320), (130, 500, None), (200, 1024, None),
+                                       (17, 2008, 2048)])
+def test_blocks_are_the_oracles_byte_for_byte(kind, R, d, pitch):
+    buf, x = _matrix(R, d, kind, seed=R + d, pitch=pitch)
+    packed = _pack(buf, kind, R, d)
+    want, _ = oo.mx4_packed(x)
+    got = packed.cpu().numpy()
+    codes = (d + 255) // 256 * 128 * R
+    # (-0 and 0 are the same value; what the sign of a zero is, is not fixed)
+    lo, hi = got & 15, got >> 4
+    wlo, whi = want & 15, want >> 4
+    for a, b in ((lo, wlo), (hi, whi)):
+        assert (np.where(a == 8, 0, a)[:codes] == np.where(b == 8, 0, b)[:codes]).all()
+    assert (got[codes:] == want[codes:]).all()
+    values = oo.mx4_blocks(x)[2]
+    for out_kind in ("f32", "bf16"):
+        dtype, dt, per = KINDS[out_kind]
+        ldo = (d + per - 1) // per * per + per
+        out = torch.full((R, ldo), 7.0, dtype=dtype, device=DEV)
+        fb.fopd_mx4_dequantize(packed, R, d, out, dt, ldo)
+        assert (out[:, :d].double().cpu().numpy() == values).all()
+        assert bool((out[:, d:] == 7.0).all())                       # columns behind the last are not written
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_every_border_between_two_values(kind):
+    """Each midpoint and its neighbours, at the ends of the range of the shared power and where it is clamped."""
+    mids = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]
+    eps = 2.0 ** -7 if kind == "bf16" else 2.0 ** -23
+    row = [4.0] + [m * f for m in mids for f in (1.0, 1.0 - eps, 1.0 + eps)] + [-m for m in mids] + [7.5, -6.5, 0.0]
+    x = torch.tensor([row + [0.0] * (32 - len(row))], dtype=torch.float64)
+    scales = [2.0 ** e for e in (-126, -125, -20, 0, 1, 60, 124)]
+    x = torch.cat([x * s for s in scales] + [torch.zeros(1, 32, dtype=torch.float64), torch.full((1, 32), 2.0 ** -130, dtype=torch.float64),
+                                             torch.full((1, 32), -3.0e38, dtype=torch.float64)])
+    buf = x.to(KINDS[kind][0]).to(DEV).contiguous()
+    R = buf.shape[0]
+    packed = _pack(buf, kind, R, 32)
+    out = torch.empty(R, 32, device=DEV)
+    fb.fopd_mx4_dequantize(packed, R, 32, out, fb.FOPD_F32, 32)
+    assert (out.double().cpu().numpy() == oo.mx4_blocks(buf.double().cpu().numpy())[2]).all()
+
+
+def test_infinities_and_nan_make_their_block_nan_and_no_other():
+    buf, x = _matrix(70, 320, "bf16", seed=5)
+    buf[3, 40] = float("inf")
+    buf[66, 0] = float("nan")
+    buf[69, 319] = float("-inf")
+    packed = _pack(buf, "bf16", 70, 320)
+    out = torch.empty(70, 320, device=DEV)
+    fb.fopd_mx4_dequantize(packed, 70, 320, out, fb.FOPD_F32, 320)
+    want = oo.mx4_blocks(buf.double().cpu().numpy())[2]
+    assert np.isnan(want).sum() == 96
+    assert np.array_equal(out.double().cpu().numpy(), want, equal_nan=True)
+    # a product with such a row is NaN, the others are not touched by it
+    w, wx = _matrix(100, 320, "bf16", seed=6)
+    z = torch.zeros(70, 104, device=DEV)
+    fb.fopd_mx4_logits(buf, fb.FOPD_BF16, 320, _pack(w, "bf16", 100, 320), 70, 100, 320, z, fb.FOPD_F32, 104,
+                       _workspace(fb.fopd_mx4_logits_workspace_bytes(70, 100, 320)))
+    nan = torch.isnan(z[:, :100])
+    assert bool(nan[[3, 66, 69]].all()) and int(nan.sum()) == 300
+
+
+def _logits(T, V, d, kind_h, kind, seed, h_pitch=None):
+    hb, hx = _matrix(T, d, kind_h, seed, spread=2, pitch=h_pitch)
+    wb, wx = _matrix(V, d, "bf16", seed + 1, spread=2)
+    packed = _pack(wb, "bf16", V, d)
+    dtype, dt, per = KINDS[kind]
+    ld = (V + per - 1) // per * per + per
+    z = torch.full((T + 1, ld), 7.0, dtype=dtype, device=DEV)
+    ws = _workspace(fb.fopd_mx4_logits_workspace_bytes(T, V, d))
+    args = (hb, KINDS[kind_h][1], hb.shape[1], packed, T, V, d, z, dt, ld, ws)
+    fb.fopd_mx4_logits(*args)
+    return z, hx, wx, args
+
+
+def _check(z, hx, wx, T, V, d, kind):
+    h, w = (torch.from_numpy(oo.mx4_blocks(m)[2]) for m in (hx, wx))
+    want, size = h @ w.t(), h.abs() @ w.abs().t()
+    # fp32 sums in any order: at most d additions of terms whose magnitudes add up to `size`, each off by at most a unit in the
+    # last place; then the rounding to the result's type
+    tol = d * 2.0 ** -23 * size + (2.0 ** -8 if kind == "bf16" else 2.0 ** -24) * want.abs() * 1.01
+    off = (z[:T, :V].double().cpu() - want).abs()
+    assert bool((off <= tol).all()), float((off / tol.clamp(min=1e-300)).max())
+    assert bool((z[:T, V:] == 7.0).all()) and bool((z[T:] == 7.0).all())
+
+
+@pytest.mark.parametrize("kind_h,kind", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("T,V,d", [(1, 1, 1), (1, 64, 256), (2, 65, 33), (15, 100, 300), (16, 1000, 512), (17, 130, 1024), (33, 255, 700),
+                                   (64, 257, 256), (65, 64, 2000), (100, 300, 520), (255, 600, 257), (256, 256, 256), (257, 513, 300), (300, 1030, 1536),
+                                   (1000, 777, 96)])
+def test_product_against_the_oracle(T, V, d, kind_h, kind):
+    z, hx, wx, _ = _logits(T, V, d, kind_h, kind, seed=T + V)
+    _check(z, hx, wx, T, V, d, kind)
+
+
+@pytest.mark.parametrize("T,V,d,kind", [(1, 151936, 256, "bf16"), (40, 40000, 1024, "bf16"), (600, 30001, 520, "f32"), (2100, 20000, 300, "bf16")])
+def test_product_of_many_tiles(T, V, d, kind):
+    z, hx, wx, _ = _logits(T, V, d, "bf16", kind, seed=T)
+    _check(z, hx, wx, T, V, d, kind)
+
+
+@pytest.mark.parametrize("T,V,d", [(3, 1000, 512), (300, 5000, 768)])
+def test_product_twice_captured_and_on_another_stream_gives_the_same_bits(T, V, d):
+    z, hx, wx, args = _logits(T, V, d, "bf16", "bf16", seed=9)
+    first = z.clone()
+    fb.fopd_mx4_logits(*args)
+    assert torch.equal(z, first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        z.fill_(7.0)
+        fb.fopd_mx4_logits(*args)
+    side.synchronize()
+    assert torch.equal(z, first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fb.fopd_mx4_logits(*args)
+    for seed in (1, 2, 3):
+        hb, hx2 = _matrix(T, d, "bf16", seed, spread=2)
+        args[0].copy_(hb)
+        z.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(z, hx2, wx, T, V, d, "bf16")
+        replayed = z.clone()
+        fb.fopd_mx4_logits(*args)
+        assert torch.equal(z, replayed)
+
+
+def test_two_products_at_once_with_a_workspace_each():
+    one, other = (_logits(T, 3000, 512, "bf16", "f32", seed=s) for T, s in ((5, 1), (270, 2)))
+    torch.cuda.synchronize()
+    want = [one[0].clone(), other[0].clone()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for (z, _, _, args), s in zip((one, other), streams):
+            with torch.cuda.stream(s):
+                fb.fopd_mx4_logits(*args)
+    torch.cuda.synchronize()
+    assert torch.equal(one[0], want[0]) and torch.equal(other[0], want[1])

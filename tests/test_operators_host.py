@@ -1,0 +1,160 @@
+"""Refusals of the operators around the loss pass: every mistake that the host can see becomes a status before a launch."""
+
+import ctypes
+
+import pytest
+import torch
+
+from paper_2605_17862_amd import binding as fb
+
+P = ctypes.c_void_p
+
+
+def test_mx4_sizes():
+    # codes: 128 bytes a row and 256 entries, rounded up to 256; scales: 512 bytes for 64 rows and 256 entries
+    assert fb.fopd_mx4_bytes(1, 1) == 256 + 512
+    assert fb.fopd_mx4_bytes(2, 256) == 256 + 512
+    assert fb.fopd_mx4_bytes(65, 257) == 65 * 256 + 2 * 2 * 512
+    assert fb.fopd_mx4_bytes(0, 64) == 0
+    assert fb.fopd_mx4_bytes(151936, 4096) == 151936 * 2048 + 2374 * 16 * 512
+    assert fb.fopd_mx4_logits_workspace_bytes(45, 151936, 4096) >= 256 + fb.fopd_mx4_bytes(45, 4096)
+
+
+def test_mx4_rejects_bad_arguments_before_launch():
+    lib = fb.load_library()
+
+    def quantize(x=4096, dt=1, R=8, d=64, ld=64, packed=8192, n=1 << 20):
+        return lib.fopd_mx4_quantize(P(x), dt, R, d, ld, P(packed), n, None)
+
+    def dequantize(packed=8192, n=1 << 20, R=8, d=64, out=4096, dt=1, ldo=64):
+        return lib.fopd_mx4_dequantize(P(packed), n, R, d, P(out), dt, ldo, None)
+
+    for call in (quantize, dequantize):
+        assert call(packed=None) == 1
+        assert call(packed=8192 + 8) == 3
+        assert call(R=-1) == 2
+        assert call(d=0) == 2
+        assert call(dt=2) == 4
+        assert call(n=fb.fopd_mx4_bytes(8, 64) - 1) == 5
+        assert call(R=0) == 0
+    assert quantize(x=None) == 1
+    assert quantize(ld=56) == 2
+    assert quantize(d=60, ld=60) == 3
+    assert quantize(x=4096 + 4) == 3
+    assert dequantize(out=None) == 1
+    assert dequantize(ldo=60) == 2
+
+    def logits(h=4096, dth=1, ldh=64, w=8192, wn=1 << 20, T=8, V=100, d=64, z=16384, dt=0, ld=100, ws=4096, wsn=1 << 20):
+        return lib.fopd_mx4_logits(P(h), dth, ldh, P(w), wn, T, V, d, P(z), dt, ld, P(ws), wsn, None)
+
+    assert logits(h=None) == 1
+    assert logits(w=None) == 1
+    assert logits(z=None) == 1
+    assert logits(dth=7) == 4
+    assert logits(dt=-1) == 4
+    assert logits(T=-1) == 2
+    assert logits(V=0) == 2
+    assert logits(ldh=32) == 2
+    assert logits(ld=96) == 2
+    assert logits(ld=101) == 3
+    assert logits(w=8192 + 4) == 3
+    assert logits(wn=fb.fopd_mx4_bytes(100, 64) - 1) == 5
+    assert logits(ws=None) == 5
+    assert logits(ws=4096 + 16) == 5
+    assert logits(wsn=fb.fopd_mx4_logits_workspace_bytes(8, 100, 64) - 1) == 5
+    assert logits(T=0) == 0
+
+
+def _verify(lib, **kw):
+    a = dict(z=4096, zd=8192, dt=1, R=8, V=64, ld=64, ldd=64, ids=4096, row=None, lens=None, B=2, K=3, tau=None, u=4096, e=4096,
+             lde=64, n=4096, oi=4096, ol=4096, om=4096, ws=4096, wsn=1 << 22)
+    a.update(kw)
+    return lib.fopd_verify_draft(P(a["z"]), P(a["zd"]), a["dt"], a["R"], a["V"], a["ld"], a["ldd"], P(a["ids"]), P(a["row"]),
+                                 P(a["lens"]), a["B"], a["K"], P(a["tau"]), P(a["u"]), P(a["e"]), a["lde"], P(a["n"]), P(a["oi"]),
+                                 P(a["ol"]), P(a["om"]), P(a["ws"]), a["wsn"], None)
+
+
+def test_verification_rejects_bad_arguments_before_launch():
+    lib = fb.load_library()
+    assert _verify(lib, z=None) == 1
+    assert _verify(lib, ids=None) == 1
+    assert _verify(lib, u=None) == 1                              # one of the two kinds of variates alone
+    assert _verify(lib, e=None) == 1
+    for out in ("n", "oi", "ol", "om"):
+        assert _verify(lib, **{out: None}) == 1
+    assert _verify(lib, dt=3) == 4
+    assert _verify(lib, V=0) == 2
+    assert _verify(lib, B=0) == 2
+    assert _verify(lib, K=-1) == 2
+    assert _verify(lib, K=1024, R=1 << 20) == 2
+    assert _verify(lib, R=7) == 2                                 # a padded batch of 2 x 4 rows
+    assert _verify(lib, R=0) == 2
+    assert _verify(lib, B=1 << 19, K=2, R=1 << 22) == 2           # more than 2^20 places
+    assert _verify(lib, ld=56) == 2
+    assert _verify(lib, ldd=56) == 2
+    assert _verify(lib, lde=60) == 2
+    assert _verify(lib, lde=66) == 3
+    assert _verify(lib, e=4096 + 4) == 3
+    assert _verify(lib, zd=8192 + 2) == 3
+    assert _verify(lib, ws=None) == 5
+    assert _verify(lib, ws=4096 + 64) == 5
+    need = fb.fopd_verify_workspace_bytes(8, 64, 2)
+    assert need % 256 == 0 and _verify(lib, wsn=need - 1) == 5
+
+
+def test_status_of_a_row_without_a_distribution():
+    assert fb.fopd_flags_status(16) == 12
+    assert fb.fopd_flags_status(17) == 6
+    assert fb.fopd_status_string(12) != "unknown status"
+
+
+def _entry(**kw):
+    a = dict(grad=4096, out=4096, rows=1, cols=64, ld=64, ld_out=64, dt=0, dt_out=0)
+    a.update(kw)
+    return fb.GradTensor(*[a[k] for k, _ in fb.GradTensor._fields_])
+
+
+def test_gradient_calls_reject_bad_arguments_before_launch():
+    lib = fb.load_library()
+
+    def norm(entries, n=None, s=4096, ws=4096, wsn=1 << 20):
+        arr = (fb.GradTensor * len(entries))(*entries)
+        return lib.fopd_grad_norm(ctypes.cast(arr, P), len(entries) if n is None else n, 0, P(s), None, P(ws), wsn, None)
+
+    def clip(entries, n=None, s=4096, most=1.0, eps=1e-6):
+        arr = (fb.GradTensor * len(entries))(*entries)
+        return lib.fopd_grad_clip(ctypes.cast(arr, P), len(entries) if n is None else n, P(s), most, eps, None, None)
+
+    good = _entry()
+    for call in (norm, clip):
+        assert call([good], n=-1) == 2
+        assert call([good], s=None) == 1
+        assert call([good, _entry(grad=None)]) == 1
+        assert call([good, _entry(dt=2)]) == 4
+        assert call([_entry(rows=2, ld=63)]) == 2
+        assert call([_entry(rows=-1)]) == 2
+        assert call([_entry(cols=1 << 41, ld=1 << 41)]) == 2
+        assert call([_entry(grad=4096 + 2, out=8192)]) == 3
+    assert lib.fopd_grad_norm(None, 1, 0, P(4096), None, P(4096), 1 << 20, None) == 1
+    assert lib.fopd_grad_clip(None, 1, P(4096), 1.0, 0.0, None, None) == 1
+    assert norm([good], ws=None) == 5
+    assert norm([good], ws=4096 + 8) == 5
+    assert norm([good], wsn=fb.fopd_grad_workspace_bytes() - 1) == 5
+    assert clip([_entry(out=None)]) == 1
+    assert clip([_entry(dt_out=5)]) == 4
+    assert clip([_entry(dt_out=1)]) == 1                          # in place, of another type
+    assert clip([_entry(rows=2, ld=64, ld_out=72)]) == 1          # in place, of another pitch
+    assert clip([_entry(out=8192, rows=2, ld_out=60)]) == 2
+    assert clip([_entry(out=8193, dt_out=1)]) == 3
+    for bad in (-1.0, float("nan")):
+        assert clip([good], most=bad) == 1
+        assert clip([good], eps=bad) == 1
+
+
+def test_gradient_list_refuses_what_it_cannot_describe():
+    for grads, outs in (([torch.zeros(4)], None),                                       # host memory
+                        ([torch.zeros(4, dtype=torch.float16)], None)):
+        with pytest.raises(ValueError):
+            fb.grad_tensors(grads, outs)
+    with pytest.raises(ValueError):
+        fb.grad_tensors([torch.zeros(4)], [])
