@@ -681,6 +681,17 @@ fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d,
 // weight [V, d] and hidden rows [T, d], both packed.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
+  if (T > 64) {
+    const int tiles_m = static_cast<int>((V + kGemmTile - 1) / kGemmTile), tiles_n = static_cast<int>((T + kGemmTile - 1) / kGemmTile);
+    const bool walk = gemm_walks(static_cast<int64_t>(tiles_m) * tiles_n, Mx4Layout(V, d).steps, false);
+    auto tiles = dt == FOPD_BF16 ? (walk ? fopd_mx4_tiles<FOPD_BF16, true> : fopd_mx4_tiles<FOPD_BF16, false>)
+                                 : (walk ? fopd_mx4_tiles<FOPD_F32, true> : fopd_mx4_tiles<FOPD_F32, false>);
+    static bool done[2][2][kMaxDevices] = {};
+    const fopd_status st = allow_dynamic_lds(reinterpret_cast<const void*>(tiles), kMxTileLds, done[dt == FOPD_BF16][walk]);
+    if (st != FOPD_OK) return st;
+    tiles<<<gemm_grid((tile_groups(tiles_m, tiles_n) + 7) / 8, walk), kLmThreads, kMxTileLds, s>>>(w, V, h, T, d, out, ldo, tiles_m, tiles_n);
+    return launched();
+  }
   const int blocks = T <= 16 ? 1 : (T <= 32 ? 2 : 4);
   const dim3 grid(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((T + 16 * blocks - 1) / (16 * blocks)));
   auto kern = dt == FOPD_BF16 ? (blocks == 1 ? fopd_mx4_few<FOPD_BF16, 1> : blocks == 2 ? fopd_mx4_few<FOPD_BF16, 2> : fopd_mx4_few<FOPD_BF16, 4>)

@@ -273,6 +273,317 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
   }
 }
 
+// ---- many rows of H: 256 x 256 tiles -------------------------------------------------------------------------------
+// The loop of fopd_lm_head.hip (matrix_step) on 4-bit operands: a row of a half tile is 128 bytes of a step there and here, 64
+// bf16 or 256 4-bit entries, the fragments are the same 16 bytes and the instruction takes as long, so what holds for the LDS
+// and the loads of that loop holds for this one; a product does four times the work.  The scales of a step are one more load
+// a wavefront, 512 bytes of the 64 rows that are its own to fetch (A's four groups of a tile, then B's four), requested with
+// B0 and, like B0, all read in the step's first slot:
+//
+//   phase   reads              multiplies   requests                              waits for (besides its own LDS reads)
+//     1     B0, A0, scales     A0 x B0      A1 of the next step
+//     2     B1                 A0 x B1      B0 and scales of the next but one     A1 of this step                    (12 loads stay in flight)
+//     3     A1                 A1 x B1      A0 of the next but one
+//     4                        A1 x B0      B1 of the next but one                B0, scales, A0, B1 of the next step    (9)
+
+constexpr int kMxScaleLds = 8 * 1024;                     // scales of a step (half of each 1 KB is not read)
+constexpr int kMxTileLds = kLoopLdsBytes + 2 * kMxScaleLds;
+
+namespace {
+
+struct MxLoader {
+  RowMajorSource a, b;
+  const RowMajorHalf& at;
+  uint32_t lds, scale_lds, scale_lane;
+  bool of_b;                                               // this wavefront fetches scales of B, else of A
+  const char* scales;                                      // of that matrix
+  int groups, group, steps;                                // its groups of 64 rows; place among the tile's four
+  const char* scale_src;
+  __device__ __forceinline__ void locate(const GemmTile& t) {
+    a.locate(at, t.m0, 0);
+    b.locate(at, t.n0, 0);
+    scale_src = scales + static_cast<int64_t>(min(((of_b ? t.n0 : t.m0) >> 6) + group, groups - 1)) * steps * kMxScaleBytes;
+  }
+  __device__ __forceinline__ void step(bool on = true) {
+    a.step(on);
+    b.step(on);
+    scale_src += on ? kMxScaleBytes : 0;
+  }
+  __device__ __forceinline__ void request(int half, int buf) {
+    const uint32_t dst = lds + buf * kStepBytes + half * kHalfBytes;
+    if (half < 2) a.request(half, dst);
+    else b.request(half - 2, dst);
+    if (half == kHalfB0) load_to_lds(scale_src, scale_lane, scale_lds + buf * kMxScaleLds);
+  }
+};
+
+typedef f32x4 MxAcc[2][4][2][2];                          // [A half][16-row block][B half][16-row block]
+
+template <int FLIGHT>
+__device__ __forceinline__ void mx_wait() {
+  static_assert(FLIGHT <= 63, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLIGHT) : "memory");
+}
+
+__device__ __forceinline__ void mx_product(MxAcc& acc, int a, int b, const i32x4 (&fa)[4][2], const i32x4 (&fb)[2][2], uint2 sa, uint32_t sb) {
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        acc[a][i][b][j] = mx_multiply(fa[i][ks], fb[j][ks], acc[a][i][b][j], static_cast<int>(i < 2 ? sa.x : sa.y), 2 * (i & 1) + ks,
+                                      static_cast<int>(sb), 2 * j + ks);
+}
+
+// STORES: stores of the tile before that are still in flight behind the requests that this step waits for (loads and stores
+// count and end in order).
+template <int STORES, typename Request>
+__device__ __forceinline__ void mx_step(MxAcc& acc, const RowMajorFragments<>& frags, const unsigned char* here, const unsigned char* scales_a,
+                                        const unsigned char* scales_b, Request request) {
+  i32x4 fa[4][2], fb0[2][2], fb1[2][2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) fb0[j][ks] = __builtin_bit_cast(i32x4, frags.b(here, 0, j, ks));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) fa[i][ks] = __builtin_bit_cast(i32x4, frags.a(here, 0, i, ks));
+  const uint2 sa0 = *reinterpret_cast<const uint2*>(scales_a), sa1 = *reinterpret_cast<const uint2*>(scales_a + 2048);
+  const uint32_t sb0 = *reinterpret_cast<const uint32_t*>(scales_b), sb1 = *reinterpret_cast<const uint32_t*>(scales_b + 2048);
+  request(kHalfA1);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  slot_end();
+  mx_product(acc, 0, 0, fa, fb0, sa0, sb0);
+  slot_end();
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) fb1[j][ks] = __builtin_bit_cast(i32x4, frags.b(here, 1, j, ks));
+  request(kHalfB0);
+  mx_wait<12 + STORES>();
+  slot_end();
+  mx_product(acc, 0, 1, fa, fb1, sa0, sb1);
+  slot_end();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) fa[i][ks] = __builtin_bit_cast(i32x4, frags.a(here, 1, i, ks));
+  request(kHalfA0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  slot_end();
+  mx_product(acc, 1, 1, fa, fb1, sa1, sb1);
+  slot_end();
+  request(kHalfB1);
+  mx_wait<9 + STORES>();
+  slot_end();
+  mx_product(acc, 1, 0, fa, fb0, sa1, sb0);
+  slot_end();
+}
+
+// Lanes 8 .. 15 of each sixteen of `low` change places with lanes 0 .. 7 of `high`.
+__device__ __forceinline__ void swap_eights(uint32_t& low, uint32_t& high) {
+  const int l = static_cast<int>(low), h = static_cast<int>(high);
+  low = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(l, h, 0x128, 0xf, 0xc, false));      // row_ror:8, lanes 8 .. 15
+  high = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(h, l, 0x128, 0xf, 0x3, false));     // lanes 0 .. 7
+}
+
+// 16 bytes of results of row t from column v on.
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void mx_store(void* out, int64_t ldo, int64_t t, int64_t v, int64_t T, int64_t V, const u32x4& q) {
+  constexpr int E = Elem<DT>::kPerVec;
+  char* o = static_cast<char*>(out) + (t * ldo + v) * Elem<DT>::kBytes;
+  if (WHOLE || (t < T && v + E <= V)) {
+    __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(o));
+  } else if (t < T) {
+    float x[E];
+    unpack<DT>(q, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (v + e < V) store_elem<DT>(o, e, x[e]);
+  }
+}
+
+// Register r of acc[a][i][b][j] is vocabulary row 128 a + 64 wm + 16 i + 4 (lane / 16) + r of the tile, row 128 b + 32 wn + 16 j +
+// lane % 16 of H's.  Lanes change places until a store writes whole 128-byte lines of eight rows, 16 bytes a lane.
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void mx_store_block(const MxAcc& acc, const MatrixPlace& place, int m0, int n0, int64_t T, int64_t V,
+                                               void* __restrict__ out, int64_t ldo) {
+  const int lane = threadIdx.x & 63, n = lane & 7, upper = (lane >> 3) & 1, q = lane >> 4;
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int64_t t = n0 + 128 * b + 32 * place.wn + 16 * j + n;
+        const int64_t v = m0 + 128 * a + 64 * place.wm;
+        if constexpr (DT == FOPD_F32) {
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            u32x4 x = __builtin_bit_cast(u32x4, acc[a][i][b][j]), y = __builtin_bit_cast(u32x4, acc[a][i + 1][b][j]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              uint32_t lo = x[r], hi = y[r];
+              swap_eights(lo, hi);
+              x[r] = lo;
+              y[r] = hi;
+            }
+            mx_store<DT, WHOLE>(out, ldo, t, v + 16 * (i + upper) + 4 * q, T, V, x);
+            mx_store<DT, WHOLE>(out, ldo, t + 8, v + 16 * (i + upper) + 4 * q, T, V, y);
+          }
+        } else {
+          u32x4 u[2];                                      // columns 8 q .. + 7 of the first and of the second 32
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const f32x4 &x = acc[a][2 * h][b][j], &y = acc[a][2 * h + 1][b][j];
+              const auto s32 = __builtin_amdgcn_permlane32_swap(pack_bf16x2(x[2 * r], x[2 * r + 1]), pack_bf16x2(y[2 * r], y[2 * r + 1]), false, false);
+              const auto s16 = __builtin_amdgcn_permlane16_swap(s32[0], s32[1], false, false);
+              u[h][r] = s16[0];
+              u[h][r + 2] = s16[1];
+            }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            uint32_t lo = u[0][r], hi = u[1][r];
+            swap_eights(lo, hi);
+            u[0][r] = lo;
+            u[1][r] = hi;
+          }
+          mx_store<DT, WHOLE>(out, ldo, t, v + 32 * upper + 8 * q, T, V, u[0]);
+          mx_store<DT, WHOLE>(out, ldo, t + 8, v + 32 * upper + 8 * q, T, V, u[1]);
+        }
+      }
+}
+
+}  // namespace
+
+// Launched as fopd_gemm_nt is (TileWalk): m the vocabulary, n the rows of H.
+template <int DT, bool WALK>
+__global__ void __launch_bounds__(kLmThreads)
+fopd_mx4_tiles(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
+               void* __restrict__ out, int64_t ldo, int tiles_m, int tiles_n) {
+  extern __shared__ __align__(16) unsigned char mx_smem[];
+  const Mx4Layout w_at(V, d), h_at(T, d);
+  const int steps = static_cast<int>(w_at.steps);
+  TileWalk<true, WALK> walk = {tiles_m, tiles_n, steps, 1};
+  GemmTile tile;
+  if (!walk.first(tile, blockIdx.x)) return;               // whole workgroup, before any barrier
+
+  const MatrixPlace mine = matrix_place(mx_smem);
+  const RowMajorHalf at(mine);
+  const RowMajorFragments<> frags(mine);
+  const int lane = threadIdx.x & 63, wave = mine.wm * 4 + mine.wn;
+  const unsigned char* scales = mx_smem + kLoopLdsBytes;
+  const unsigned char* scales_a = scales + mine.wm * 1024 + lane * 8;
+  const unsigned char* scales_b = scales + (4 + (mine.wn >> 1)) * 1024 + lane * 8 + (mine.wn & 1) * 4;
+  MxLoader load = {{}, {}, at, mine.lds, mine.lds - wave * 2048u + kLoopLdsBytes + wave * 1024u, (lane & 31) * 16u,
+                   wave >= 4, reinterpret_cast<const char*>(wave >= 4 ? H + h_at.codes : W + w_at.codes),
+                   static_cast<int>(wave >= 4 ? h_at.groups : w_at.groups), wave & 3, steps, nullptr};
+  load.a.base = reinterpret_cast<const char*>(W);
+  load.a.ld = load.b.ld = w_at.steps * (kMxRowBytes / 2);  // (the source counts in 2-byte entries)
+  load.a.rows = static_cast<int>(V);
+  load.b.base = reinterpret_cast<const char*>(H);
+  load.b.rows = static_cast<int>(T);
+
+  // the stream of steps, as matrix_tiles
+  constexpr int kStores = DT == FOPD_F32 ? 32 : 16;        // of a whole tile, by a wavefront
+  GemmTile ahead_tile = tile;
+  TileWalk<true, WALK> ahead = walk;
+  int left = steps;
+  load.locate(tile);
+  auto advance = [&]() {
+    if constexpr (!WALK) {
+      const bool more = left > 1;
+      left -= more ? 1 : 0;
+      load.step(more);
+    } else if (--left > 0) {
+      load.step();
+    } else if (ahead.next(ahead_tile)) {
+      left = steps;
+      load.locate(ahead_tile);
+    } else {
+      left = 1;                                            // the last step again, never read
+    }
+  };
+#pragma unroll
+  for (int buf = 0; buf < 2; ++buf) {
+    load.request(kHalfB0, buf);
+    load.request(kHalfA0, buf);
+    load.request(kHalfB1, buf);
+    if (buf == 0) {
+      load.request(kHalfA1, buf);
+      advance();
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+  slot_end();
+  if (mine.wm == 1) slot_end();
+  int cur = 0;
+  bool stored = false;
+  MxAcc acc;
+  while (true) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[h][i][b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto run = [&](auto stores_tag, auto switch_tag) {
+      mx_step<decltype(stores_tag)::value>(acc, frags, mx_smem + cur * kStepBytes, scales_a + cur * kMxScaleLds, scales_b + cur * kMxScaleLds,
+                                           [&](int half) {
+        load.request(half, half == kHalfA1 ? 1 - cur : cur);
+        if (half == kHalfA1) {
+          if constexpr (decltype(switch_tag)::value) {
+            advance();
+          } else {
+            --left;
+            load.step();
+          }
+        }
+      });
+      cur = 1 - cur;
+    };
+    typedef std::integral_constant<int, 0> None;
+    typedef std::integral_constant<int, kStores> Some;
+    int kt = steps;
+    if constexpr (!WALK) {
+      for (; kt > 0; --kt) run(None(), std::true_type());
+      matrix_end(mine);
+      if (tile.m0 + kGemmTile <= V && tile.n0 + kGemmTile <= T) mx_store_block<DT, true>(acc, mine, tile.m0, tile.n0, T, V, out, ldo);
+      else mx_store_block<DT, false>(acc, mine, tile.m0, tile.n0, T, V, out, ldo);
+      return;
+    }
+    if (stored) {
+      if (left > 1) run(Some(), std::false_type());
+      else run(Some(), std::true_type());
+      --kt;
+    }
+    while (kt > 0) {
+      const int plain = min(kt, left - 1);
+      for (int i = 0; i < plain; ++i) run(None(), std::false_type());
+      kt -= plain;
+      if (kt > 0) {
+        run(None(), std::true_type());
+        --kt;
+      }
+    }
+    stored = tile.m0 + kGemmTile <= V && tile.n0 + kGemmTile <= T;
+    if (stored) {
+      mx_store_block<DT, true>(acc, mine, tile.m0, tile.n0, T, V, out, ldo);
+    } else {                                               // an unknown number of stores: waited for
+      mx_store_block<DT, false>(acc, mine, tile.m0, tile.n0, T, V, out, ldo);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    if (!walk.next(tile)) break;
+  }
+  matrix_end(mine);
+}
+
 }  // namespace fopd
 
 #endif  // FOPD_MX4_HIP_
