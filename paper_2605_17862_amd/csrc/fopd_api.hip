@@ -702,20 +702,20 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
 
 // ---- verification of drafted tokens ---------------------------------------------------------
 
-// How a call is cut: pieces of a row in the first kernel (a power of two), pieces of a race.  Both go by sizes that the workspace
-// is asked for with, so neither depends on the type or on the lengths.
+// How a call is cut: pieces of a row in the first kernel (a power of two), pieces of a race.  The workspace is asked for with R, V
+// and B, so `splits` is the most that a call of any number of drafts may take.
 struct VerifyPlan {
   int splits, pieces;
-  size_t parts, races, verdicts, total;
+  size_t parts, drafted, races, total;
   VerifyPlan(int64_t R, int64_t V, int32_t B) {
     const int64_t rows = R < 1 ? 1 : R, samples = B < 1 ? 1 : B;
     splits = 1;
-    while (splits < kVerifyMaxSplits && splits * rows < 4096 && V / (2 * splits) >= 2048) splits *= 2;
-    pieces = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((V + 2047) / 2048, 2048 / samples)));
+    while (splits < kVerifyMaxSplits && splits * rows < 2048 && V / (2 * splits) >= 2048) splits *= 2;
+    pieces = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((V + 4095) / 4096, 16), 1024 / samples)));
     size_t off = 256;
     parts = Workspace::take(off, 2 * static_cast<size_t>(rows) * splits * sizeof(RowPart));
-    races = Workspace::take(off, static_cast<size_t>(samples) * pieces * sizeof(RacePart));
-    verdicts = Workspace::take(off, static_cast<size_t>(samples) * sizeof(Verdict));
+    drafted = Workspace::take(off, 2 * static_cast<size_t>(rows) * sizeof(float));
+    races = Workspace::take(off, static_cast<size_t>(samples) * sizeof(RaceState));
     total = off;
   }
 };
@@ -724,16 +724,17 @@ template <int DT>
 fopd_status launch_verify(const VerifyArgs& a, const VerifyPlan& plan, void* ws, hipStream_t s) {
   const int nvec = a.V / Elem<DT>::kPerVec;
   const unsigned units = static_cast<unsigned>(a.B) * static_cast<unsigned>(a.K + 1) * (a.draft != nullptr ? 2u : 1u);
-  int splits = plan.splits;                                // (many places for few rows: a launch has at most 2^32 lanes)
-  while (splits > 1 && static_cast<int64_t>(units) * splits > kLaunchRows * 4) splits /= 2;
+  int splits = 1;
+  while (splits < plan.splits && static_cast<int64_t>(units) * splits < 768) splits *= 2;
+  const int64_t cached = (200LL << 20) / (static_cast<int64_t>(a.V) * Elem<DT>::kBytes) * splits, groups = static_cast<int64_t>(units) * splits;
   RowPart* parts = at<RowPart>(ws, plan.parts);
-  RacePart* races = at<RacePart>(ws, plan.races);
-  Verdict* verdicts = at<Verdict>(ws, plan.verdicts);
+  RaceState* races = at<RaceState>(ws, plan.races);
+  float* drafted = at<float>(ws, plan.drafted);
   int32_t* flags = at<int32_t>(ws, 0);
-  fopd_verify_rows<DT><<<units * splits, kVerifyThreads, 0, s>>>(a, splits, (nvec + splits - 1) / splits, parts);
+  fopd_verify_rows<DT><<<static_cast<unsigned>(groups), kVerifyThreads, 0, s>>>(a, splits, (nvec + splits - 1) / splits, parts, drafted, races,
+                                                            static_cast<unsigned>(std::max<int64_t>(0, groups - cached)));
   fopd_verify_race<DT><<<static_cast<unsigned>(a.B) * plan.pieces, kVerifyThreads, 2 * (a.K + 1) * sizeof(RowPart), s>>>(
-      a, splits, parts, plan.pieces, (nvec + plan.pieces - 1) / plan.pieces, races, verdicts, flags);
-  fopd_verify_finish<DT><<<static_cast<unsigned>(a.B), 64, 0, s>>>(a, plan.pieces, races, verdicts, flags);
+      a, splits, parts, drafted, plan.pieces, (nvec + plan.pieces - 1) / plan.pieces, races, flags);
   return launched();
 }
 
