@@ -755,7 +755,7 @@ fopd_status check_grad_tensor(const fopd_grad_tensor& t, bool with_out) {
   return FOPD_OK;
 }
 
-// launch(table) for the tensors of a list, kGradTable of them or kGradMaxPieces pieces at a time.
+// launch(table) for the tensors of a list, kGradTable of them or kGradMaxPieces pieces at a time; with outputs from the last on.
 template <typename Launch>
 fopd_status grad_tables(const fopd_grad_tensor* tensors, int32_t n, bool with_out, Launch launch) {
   GradTable g;
@@ -767,14 +767,14 @@ fopd_status grad_tables(const fopd_grad_tensor* tensors, int32_t n, bool with_ou
     return st;
   };
   for (int32_t i = 0; i < n; ++i) {
-    const fopd_grad_tensor& t = tensors[i];
+    const fopd_grad_tensor& t = tensors[with_out ? n - 1 - i : i];
     if (t.rows == 0 || t.cols == 0) continue;
     int64_t rows = t.rows, cols = t.cols;
     if (t.ld == t.cols && (!with_out || t.ld_out == t.cols)) {          // no gaps: one row
       cols *= rows;
       rows = 1;
     }
-    const int64_t row_pieces = (cols + kGradPiece - 1) / kGradPiece;
+    const int64_t piece = kGradPieceBytes >> (t.dt == FOPD_BF16 ? 1 : 2), row_pieces = (cols + piece - 1) / piece;
     if (row_pieces > kGradMaxPieces) return FOPD_ESHAPE;
     for (int64_t r = 0; r < rows;) {
       const int64_t here = std::min(rows - r, std::max<int64_t>(1, kGradMaxPieces / row_pieces));
@@ -2036,13 +2036,17 @@ fopd_status fopd_grad_norm(const fopd_grad_tensor* tensors_host, int32_t n, int 
     add = true;
     return launched();
   };
+  int64_t pieces = 0;                                      // of the tables to come
+  for (int32_t i = 0; i < n; ++i) pieces += tensors_host[i].rows * tensors_host[i].cols / (kGradPieceBytes >> (tensors_host[i].dt == FOPD_BF16 ? 1 : 2));
   const fopd_status st = grad_tables(tensors_host, n, false, [&](const GradTable& g) {
+    const int64_t first_cached = std::min<int64_t>(std::max<int64_t>(0, pieces - (200LL << 20) / kGradPieceBytes), g.pieces);
+    pieces -= g.pieces;
     const int grid = std::min(g.pieces, kGradGrid);
     if (used + grid > kGradPartials) {
       const fopd_status full = finish(nullptr);
       if (full != FOPD_OK) return full;
     }
-    fopd_grad_sum_squares<<<static_cast<unsigned>(grid), kGradLanes, 0, s>>>(g, partial + used);
+    fopd_grad_sum_squares<<<static_cast<unsigned>(grid), kGradLanes, 0, s>>>(g, partial + used, static_cast<int>(first_cached));
     used += grid;
     return launched();
   });

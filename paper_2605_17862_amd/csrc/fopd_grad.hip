@@ -10,7 +10,9 @@
 //
 // A launch gets up to kGradTable tensors by value, in its kernel arguments: nothing is copied to the device beforehand, and a
 // captured launch keeps its own table.  A tensor is rows of `cols` entries; rows that follow each other without a gap are one
-// long row.  It is cut into pieces of kGradPiece entries of a row, dealt to the workgroups in turn.
+// long row.  It is cut into pieces of kGradPieceBytes of a row, dealt to the workgroups in turn; a lane has all 16-byte loads of a
+// piece in flight at once.  The norm goes through the list from the front, the scaling from the back: what the norm read
+// last is still in the Infinity Cache.
 
 #ifndef FOPD_GRAD_HIP_
 #define FOPD_GRAD_HIP_
@@ -23,8 +25,9 @@
 namespace fopd {
 
 constexpr int kGradTable = 48;
-constexpr int kGradPiece = 8192;              // entries: 16 or 32 KB
+constexpr int kGradPieceBytes = 32768;
 constexpr int kGradLanes = 256;
+constexpr int kGradVecs = kGradPieceBytes / 16 / kGradLanes;
 constexpr int kGradMaxGroups = 4096;          // workgroups of a launch of fopd_grad_sum_squares
 constexpr int64_t kGradMaxPieces = 1LL << 30; // pieces of a launch
 
@@ -62,35 +65,52 @@ __device__ __forceinline__ int grad_tensor_of(const GradTable& g, int piece) {
 __device__ __forceinline__ GradPlace grad_place(const GradEntry& t, int piece) {
   const int local = piece - t.first_piece;
   const int row = local / t.row_pieces;
-  const int64_t col = static_cast<int64_t>(local - row * t.row_pieces) * kGradPiece;
+  const int most = kGradPieceBytes >> (t.bf16 ? 1 : 2);
+  const int64_t col = static_cast<int64_t>(local - row * t.row_pieces) * most;
   const int64_t left = t.cols - col;
-  return GradPlace{row, col, static_cast<int>(left < kGradPiece ? left : kGradPiece)};
+  return GradPlace{row, col, static_cast<int>(left < most ? left : most)};
 }
 
-template <int DT>
-__device__ __forceinline__ double grad_piece_squares(const char* p, int count) {
-  constexpr int E = Elem<DT>::kPerVec, B = Elem<DT>::kBytes;
-  const int tid = threadIdx.x;
-  // entries up to the first 16-byte boundary, then vectors, then the rest
-  const int head = min(count, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / B);
-  const int nvec = (count - head) / E;
-  double a[4] = {0.0, 0.0, 0.0, 0.0};
-  if (tid < head) {
-    const double x = load_elem<DT>(p, tid);
-    a[0] = fma(x, x, a[0]);
+// Calls with the vectors' 16-byte loads all under way: body(vector, its value), vectors first + lane + 256 u.
+template <bool CACHED, typename Body>
+__device__ __forceinline__ void grad_vectors(const u32x4* v, int n, Body body) {
+  u32x4 q[kGradVecs];
+  if (n == kGradVecs * kGradLanes) {
+#pragma unroll
+    for (int u = 0; u < kGradVecs; ++u) q[u] = load_vec<CACHED>(v + threadIdx.x + u * kGradLanes);
+#pragma unroll
+    for (int u = 0; u < kGradVecs; ++u) body(static_cast<int>(threadIdx.x) + u * kGradLanes, q[u]);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kGradVecs; ++u)
+      if (static_cast<int>(threadIdx.x) + u * kGradLanes < n) q[u] = load_vec<CACHED>(v + threadIdx.x + u * kGradLanes);
+#pragma unroll
+    for (int u = 0; u < kGradVecs; ++u)
+      if (static_cast<int>(threadIdx.x) + u * kGradLanes < n) body(static_cast<int>(threadIdx.x) + u * kGradLanes, q[u]);
   }
-  const u32x4* v = reinterpret_cast<const u32x4*>(p + head * B);
-#pragma unroll 4
-  for (int j = tid; j < nvec; j += kGradLanes) {
+}
+
+// Entries before the first 16-byte boundary.
+template <int DT>
+__device__ __forceinline__ int grad_head(const char* p, int count) {
+  return min(count, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / Elem<DT>::kBytes);
+}
+
+template <int DT, bool CACHED>
+__device__ __forceinline__ double grad_piece_squares(const char* p, int count) {
+  constexpr int E = Elem<DT>::kPerVec;
+  const int tid = threadIdx.x, head = grad_head<DT>(p, count), nvec = (count - head) / E;
+  double a[4] = {0.0, 0.0, 0.0, 0.0};
+  grad_vectors<CACHED>(reinterpret_cast<const u32x4*>(p + head * Elem<DT>::kBytes), nvec, [&](int, const u32x4& q) {
     float x[E];
-    unpack<DT>(v[j], x);
+    unpack<DT>(q, x);
 #pragma unroll
     for (int e = 0; e < E; ++e) a[e & 3] = fma(static_cast<double>(x[e]), static_cast<double>(x[e]), a[e & 3]);
-  }
-  const int rest = head + nvec * E + tid;
-  if (rest < count) {
-    const double x = load_elem<DT>(p, rest);
-    a[1] = fma(x, x, a[1]);
+  });
+  const int rest = count - nvec * E;           // fewer than two vectors' entries, before and behind them
+  if (tid < rest) {
+    const double x = load_elem<DT>(p, tid < head ? tid : nvec * E + tid);
+    a[0] = fma(x, x, a[0]);
   }
   return (a[0] + a[1]) + (a[2] + a[3]);
 }
@@ -98,46 +118,48 @@ __device__ __forceinline__ double grad_piece_squares(const char* p, int count) {
 template <int DT, int DT_OUT>
 __device__ __forceinline__ void grad_piece_scale(const char* p, char* o, int count, float c) {
   constexpr int E = Elem<DT>::kPerVec, B = Elem<DT>::kBytes, BO = Elem<DT_OUT>::kBytes;
-  const int tid = threadIdx.x;
-  // vectors of E entries on both sides where input and output reach their boundaries at the same entry
-  int head = min(count, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / B);
-  const bool wide = ((reinterpret_cast<uintptr_t>(o) + head * BO) & (E * BO < 16 ? E * BO - 1 : 15)) == 0;
-  if (!wide) {
+  const int tid = threadIdx.x, head = grad_head<DT>(p, count);
+  // vectors on both sides where input and output reach their boundaries at the same entry
+  if (((reinterpret_cast<uintptr_t>(o) + head * BO) & (E * BO < 16 ? E * BO - 1 : 15)) != 0) {
     for (int k = tid; k < count; k += kGradLanes) store_elem<DT_OUT>(o, k, c * load_elem<DT>(p, k));
     return;
   }
   const int nvec = (count - head) / E;
-  if (tid < head) store_elem<DT_OUT>(o, tid, c * load_elem<DT>(p, tid));
-  const u32x4* v = reinterpret_cast<const u32x4*>(p + head * B);
   char* ov = o + head * BO;
-#pragma unroll 4
-  for (int j = tid; j < nvec; j += kGradLanes) {
+  grad_vectors<false>(reinterpret_cast<const u32x4*>(p + head * B), nvec, [&](int j, const u32x4& q) {
     float x[E];
-    unpack<DT>(v[j], x);
+    unpack<DT>(q, x);
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= c;
     if constexpr (E * BO == 8) {
-      reinterpret_cast<uint2*>(ov)[j] = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      __builtin_nontemporal_store(u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])}, reinterpret_cast<u32x2*>(ov) + j);
     } else {
 #pragma unroll
-      for (int h = 0; h < E * BO / 16; ++h) reinterpret_cast<u32x4*>(ov)[j * (E * BO / 16) + h] = pack<DT_OUT>(x + h * (16 / BO));
+      for (int h = 0; h < E * BO / 16; ++h)
+        __builtin_nontemporal_store(pack<DT_OUT>(x + h * (16 / BO)), reinterpret_cast<u32x4*>(ov) + j * (E * BO / 16) + h);
     }
+  });
+  const int rest = count - nvec * E;
+  if (tid < rest) {
+    const int k = tid < head ? tid : nvec * E + tid;
+    store_elem<DT_OUT>(o, k, c * load_elem<DT>(p, k));
   }
-  const int rest = head + nvec * E + tid;
-  if (rest < count) store_elem<DT_OUT>(o, rest, c * load_elem<DT>(p, rest));
 }
 
 }  // namespace
 
+// Pieces from first_cached on stay in the Infinity Cache.
 __global__ void __launch_bounds__(kGradLanes)
-fopd_grad_sum_squares(GradTable g, double* __restrict__ partial) {
+fopd_grad_sum_squares(GradTable g, double* __restrict__ partial, int first_cached) {
   double sum = 0.0;
   for (int piece = blockIdx.x; piece < g.pieces; piece += gridDim.x) {
     const GradEntry& t = g.t[grad_tensor_of(g, piece)];
     const GradPlace at = grad_place(t, piece);
     const int64_t first = at.row * t.ld + at.col;
-    if (t.bf16) sum += grad_piece_squares<FOPD_BF16>(static_cast<const char*>(t.grad) + first * 2, at.count);
-    else sum += grad_piece_squares<FOPD_F32>(static_cast<const char*>(t.grad) + first * 4, at.count);
+    const char* p = static_cast<const char*>(t.grad) + first * (t.bf16 ? 2 : 4);
+    if (piece >= first_cached) sum += t.bf16 ? grad_piece_squares<FOPD_BF16, true>(p, at.count) : grad_piece_squares<FOPD_F32, true>(p, at.count);
+    else sum += t.bf16 ? grad_piece_squares<FOPD_BF16, false>(p, at.count) : grad_piece_squares<FOPD_F32, false>(p, at.count);
   }
   __shared__ double sh[kGradLanes / 64];
   sum = block_sum<kGradLanes>(sum, sh);
@@ -167,7 +189,7 @@ __global__ void __launch_bounds__(kGradLanes)
 fopd_grad_scale(GradTable g, const double* __restrict__ sum_sq, float max_norm, float eps, float* __restrict__ coef) {
   const float c = grad_coefficient(sum_sq[0], max_norm, eps);
   if (coef != nullptr && blockIdx.x == 0 && threadIdx.x == 0) coef[0] = c;
-  for (int piece = blockIdx.x; piece < g.pieces; piece += gridDim.x) {
+  for (int piece = g.pieces - 1 - static_cast<int>(blockIdx.x); piece >= 0; piece -= static_cast<int>(gridDim.x)) {
     const GradEntry& t = g.t[grad_tensor_of(g, piece)];
     if (c == 1.f && t.out == t.grad) continue;               // in place and not clipped: as it is
     const GradPlace at = grad_place(t, piece);
