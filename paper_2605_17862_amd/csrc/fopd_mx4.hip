@@ -166,21 +166,26 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
   const int64_t group = first_group + in_launch;
   const int step = static_cast<int>(blockIdx.x - in_launch * steps);
   const int tid = threadIdx.x, part = tid & 31;
-  const int64_t col = static_cast<int64_t>(step) * kMxStep + part * 8;
+  const int64_t col = static_cast<int64_t>(step) * kMxStep + part * 8, row0 = group * 64 + (tid >> 5);
   __shared__ __align__(16) unsigned char scales[kMxScaleBytes];
+  uint32_t codes[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const int64_t r = row0 + 8 * u < R ? row0 + 8 * u : R - 1;
+    codes[u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(packed + (r * at.steps + step) * kMxRowBytes) + part);
+  }
   if (tid < kMxScaleBytes / 16)
     reinterpret_cast<u32x4*>(scales)[tid] = reinterpret_cast<const u32x4*>(packed + at.codes + (group * at.steps + step) * kMxScaleBytes)[tid];
   __syncthreads();
+  if (col >= d) return;
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
-    const int in_group = (tid >> 5) + 8 * u;
-    const int64_t r = group * 64 + in_group;
-    if (r >= R || col >= d) continue;
-    const uint32_t codes = reinterpret_cast<const uint32_t*>(packed + (r * at.steps + step) * kMxRowBytes)[part];
-    const int scale = scales[mx_scale_at(in_group, part >> 2)];
+    const int64_t r = row0 + 8 * u;
+    if (r >= R) break;
+    const int scale = scales[mx_scale_at((tid >> 5) + 8 * u, part >> 2)];
     const float unit = scale == 255 ? __builtin_nanf("") : __uint_as_float(scale == 0 ? 0x00400000u : static_cast<uint32_t>(scale) << 23);
-    const f32x2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 1);
-    const f32x2v p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 3);
+    const f32x2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 1);
+    const f32x2v p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 3);
     const float x[8] = {p0.x * unit, p0.y * unit, p1.x * unit, p1.y * unit, p2.x * unit, p2.y * unit, p3.x * unit, p3.y * unit};
     char* o = static_cast<char*>(out) + (r * ldo + col) * Elem<DT>::kBytes;
     if (col + 8 <= d) {
