@@ -602,13 +602,14 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
  * 32 neighbouring entries of a row share a power of two: x_k is held as 2^s e_k with e_k one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
  * its sign (E2M1), s = max(floor(log2 max|x|) - 2, -127) (E8M0).  Entries are rounded to nearest, ties to even, and entries past
  * 6 2^s to 6 2^s (MX 1.0's rule for the scale puts the largest one at 4 .. 7.99).  A block that holds an infinity or a NaN is
- * held as 32 NaN.  d need not be a multiple of 32: the last block is shorter.
+ * held as 32 NaN.  d, at most 2^24, need not be a multiple of 32: the last block is shorter.
  *
- * A packed matrix is one buffer of fopd_mx4_bytes(R, d) bytes, 16-byte aligned, written whole by fopd_mx4_quantize:
- *   codes   row by row, ceil(d / 256) x 128 bytes a row, entry k in half k % 2 (0: the low one) of byte k / 2, zeros behind
- *           entry d - 1; then up to the next multiple of 256 bytes nothing
- *   scales  s + 127 of block b (32 entries) of row r at byte ((r / 64) ceil(d / 256) + b / 8) 512 +
- *           8 (16 (b % 4) + r % 16) + 2 (r / 16 % 4) + b / 4 % 2 behind that; 255 marks a block of NaN
+ * A packed matrix is one buffer of fopd_mx4_bytes(R, d) bytes, 16-byte aligned, written whole by fopd_mx4_quantize.  64 rows and 256
+ * columns of it are 8704 bytes, at ((r / 64) ceil(d / 256) + k / 256) 8704 for entry k of row r; with r and k counted
+ * within them from here on,
+ *   the entry's 4 bits  are in byte ((r / 16) 2 + k / 128) 1024 + (16 (k / 32 % 4) + r % 16) 16 + k % 32 / 2, the high half for odd k
+ *   its block's s + 127 is byte 8192 + 8 (16 (k / 32 % 4) + r % 16) + 2 (r / 16) + k / 128; 255 marks a block of NaN
+ * Entries and blocks that do not exist are zeros.  (The order in which the matrix cores take them: a load is a kilobyte in a row.)
  *
  * fopd_mx4_quantize    in [R, ld] of `dt` -> packed; columns d .. ld - 1 are not read
  * fopd_mx4_dequantize  packed -> out [R, ldo] of `dt`; every value that a block of bf16 entries gives is exact in bf16

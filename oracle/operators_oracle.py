@@ -36,22 +36,18 @@ def mx4_blocks(x):
 
 
 def mx4_packed(x):
-    """The packed matrix byte by byte, as the header describes it (bytes between codes and scales: 0)."""
+    """The packed matrix byte by byte, as the header describes it."""
     codes, exps, _ = mx4_blocks(x)
     R, d = codes.shape
-    steps = (d + 255) // 256
-    row = np.zeros((R, steps * 256), np.uint8)
-    row[:, :d] = codes
-    row = row[:, 0::2] | (row[:, 1::2] << 4)
-    n_codes = (R * steps * 128 + 255) // 256 * 256
-    groups = (R + 63) // 64
-    out = np.zeros(n_codes + groups * steps * 512, np.uint8)
-    out[:R * steps * 128] = row.reshape(-1)
-    for r in range(R):
-        for b in range(exps.shape[1]):
-            at = n_codes + ((r // 64) * steps + b // 8) * 512 + 8 * (16 * (b % 4) + r % 16) + 2 * (r // 16 % 4) + b // 4 % 2
-            out[at] = exps[r, b]
-    return out, n_codes
+    steps, groups = (d + 255) // 256, (R + 63) // 64
+    out = np.zeros(groups * steps * 8704, np.uint8)
+    for row in range(R):
+        for col in range(d):
+            r, k = row % 64, col % 256
+            base = ((row // 64) * steps + col // 256) * 8704
+            out[base + (r // 16 * 2 + k // 128) * 1024 + (16 * (k // 32 % 4) + r % 16) * 16 + k % 32 // 2] |= codes[row, col] << (4 * (k % 2))
+            out[base + 8192 + 8 * (16 * (k // 32 % 4) + r % 16) + 2 * (r // 16) + k // 128] = exps[row, col // 32]
+    return out
 
 
 def verify(target, draft, draft_ids, first_rows, lens, taus, u, noise):

@@ -9,13 +9,15 @@
 // largest magnitude less 2, which puts that entry at 4 .. 7.99; entries are rounded to nearest, ties to even, those past 6 to 6.
 // A block with an infinity or a NaN has s = 255, and all its values are NaN.
 //
-// A packed matrix of R rows of d entries (Mx4Layout):
-//   codes    row by row, two entries a byte, the first in the low half; a row is padded with zeros to whole steps of 256
-//            entries = 128 bytes, which is a half tile's row of one step of the loop in fopd_lm_head.hip
-//   scales   for 64 rows and a step 512 bytes: byte 8 (16 q + row % 16) + 2 (row / 16 % 4) + h is that of the row's block
-//            4 h + q of the step.  In v_mfma_scale_f32_16x16x128_f8f6f4 lane 16 q + r holds row r, entries 32 q .. + 31 of 128, so the
-//            8 bytes of a lane are the scales of its four fragments of 64 rows in both halves of the step: one LDS read of 8
-//            bytes where bytes in the order of the matrix would take 8 reads and a shift each.
+// A packed matrix of R rows of d entries is in the order in which wavefronts take it.  64 rows and a step of 256 entries are 8704
+// bytes, one step of the rows after the other, then the next 64 rows, zeros in the place of entries that do not exist:
+//   codes    in v_mfma_scale_f32_16x16x128_f8f6f4 lane 16 q + r holds row r, entries 32 q .. + 31 of 128, in 16 bytes, two entries a
+//            byte, the first in the low half.  These fragments follow each other lane by lane, 1 KB each: rows 0 - 15 with
+//            entries 0 - 127 of the step, with 128 - 255, rows 16 - 31, ..
+//   scales   512 bytes: byte 8 (16 q + r % 16) + 2 (r / 16) + h is that of row r's block 4 h + q of the step: the 8 bytes of a lane are
+//            the scales of its fragments, one read where bytes in the order of the matrix would take eight and a shift each.
+// A load of a wavefront is then 1 KB in a row, and lies in the LDS as it is read from there, free of bank conflicts.  (Rows of codes
+// one after the other, whose fragments are 64-byte pieces of sixteen rows: one row x [151,936, 4096] 69 us.)
 
 #ifndef FOPD_MX4_HIP_
 #define FOPD_MX4_HIP_
@@ -33,15 +35,17 @@
 namespace fopd {
 
 constexpr int kMxStep = 256;                  // entries of a step
-constexpr int kMxRowBytes = 128;              // code bytes of a row and step
-constexpr int kMxScaleBytes = 512;            // scale bytes of 64 rows and a step
+constexpr int kMxFragment = 1024;             // bytes of 16 rows of 128 entries
+constexpr int kMxCodeBytes = 8192;            // of 64 rows and a step
+constexpr int kMxScaleBytes = 512;
+constexpr int kMxStepBytes = kMxCodeBytes + kMxScaleBytes;
 constexpr int kMxThreads = 256;
+constexpr int64_t kMxMaxEntries = 1 << 24;     // of a row: its packed bytes are counted in 32 bits
 
 struct Mx4Layout {
-  int64_t rows, steps, groups, codes, total;  // groups of 64 rows; bytes of the codes (the scales start there) and of all
+  int64_t steps, groups, total;               // groups of 64 rows; bytes
   __host__ __device__ Mx4Layout(int64_t R, int64_t d)
-      : rows(R), steps((d + kMxStep - 1) / kMxStep), groups((R + 63) / 64),
-        codes((R * steps * kMxRowBytes + 255) / 256 * 256), total(codes + groups * steps * kMxScaleBytes) {}
+      : steps((d + kMxStep - 1) / kMxStep), groups((R + 63) / 64), total(groups * steps * kMxStepBytes) {}
 };
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -49,10 +53,11 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 namespace {
 
-// Place of the scale of block `block` (of the row) in the 512 bytes of its 64 rows and step.
-__host__ __device__ __forceinline__ int mx_scale_at(int row, int block) {
-  return 8 * (16 * (block & 3) + (row & 15)) + 2 * ((row >> 4) & 3) + ((block >> 2) & 1);
+// Places in the bytes of 64 rows and a step: of entry k of a row (the byte that holds it), and of the scale of its block b.
+__host__ __device__ __forceinline__ int mx_code_at(int row, int k) {
+  return ((row >> 4) * 2 + (k >> 7)) * kMxFragment + (16 * ((k >> 5) & 3) + (row & 15)) * 16 + ((k & 31) >> 1);
 }
+__host__ __device__ __forceinline__ int mx_scale_at(int row, int b) { return kMxCodeBytes + 8 * (16 * (b & 3) + (row & 15)) + 2 * (row >> 4) + (b >> 2); }
 
 // acc += A B over 128 entries; the scales are bytes SA of sa and SB of sb.
 template <int SA, int SB>
@@ -87,7 +92,7 @@ __device__ __forceinline__ f32x4 mx_multiply(const i32x4& a, const i32x4& b, con
 }  // namespace
 
 // Workgroup (group - first_group) x steps + step: 64 rows of one step, sixteen a wavefront.  A block is 32 / E neighbouring lanes of E entries.
-// Columns d and on are zeros and are not read; rows past the last leave scales of 0 behind.
+// Columns d and on are zeros and are not read; so are rows past the last.
 template <int DT>
 __global__ void __launch_bounds__(kMxThreads)
 fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, unsigned char* __restrict__ packed, int64_t first_group) {
@@ -99,7 +104,7 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int part = lane % kLanesPerRow;                    // of a row's step
   const int64_t col = static_cast<int64_t>(step) * kMxStep + part * E;
-  __shared__ __align__(16) unsigned char scales[kMxScaleBytes];
+  __shared__ __align__(16) unsigned char bytes[kMxStepBytes];
   const int row0 = wave * 16 + lane / kLanesPerRow;
   u32x4 q[16 / kRows];
 #pragma unroll
@@ -120,7 +125,6 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
 #pragma unroll
   for (int u = 0; u < 16 / kRows; ++u) {
     const int in_group = row0 + u * kRows;
-    const int64_t r = group * 64 + in_group;
     float x[E];
     unpack<DT>(q[u], x);
     uint32_t top = 0;                                      // magnitudes order as their bits do, infinities and NaN above the rest
@@ -143,16 +147,14 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
       codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * inv, x[3] * inv, 1.f, 1);
     }
     if (exponent == 255) codes = 0;
-    if (r < R) {
-      unsigned char* row = packed + (r * at.steps + step) * kMxRowBytes;
-      if constexpr (E == 8) reinterpret_cast<uint32_t*>(row)[part] = codes;
-      else reinterpret_cast<uint16_t*>(row)[part] = static_cast<uint16_t>(codes);
-    }
-    if (part % (32 / E) == 0) scales[mx_scale_at(in_group, part / (32 / E))] = static_cast<unsigned char>(scale);
+    unsigned char* to = bytes + mx_code_at(in_group, part * E);
+    if constexpr (E == 8) *reinterpret_cast<uint32_t*>(to) = codes;
+    else *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(codes);
+    if (part % (32 / E) == 0) bytes[mx_scale_at(in_group, part / (32 / E))] = static_cast<unsigned char>(scale);
   }
   __syncthreads();
-  if (tid < kMxScaleBytes / 16)
-    reinterpret_cast<u32x4*>(packed + at.codes + (group * at.steps + step) * kMxScaleBytes)[tid] = reinterpret_cast<const u32x4*>(scales)[tid];
+  u32x4* out = reinterpret_cast<u32x4*>(packed + (group * at.steps + step) * kMxStepBytes);
+  for (int k = tid; k < kMxStepBytes / 16; k += kMxThreads) __builtin_nontemporal_store(reinterpret_cast<const u32x4*>(bytes)[k], out + k);
 }
 
 // Workgroup (group - first_group) x steps + step, eight entries a lane.
@@ -167,25 +169,21 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
   const int step = static_cast<int>(blockIdx.x - in_launch * steps);
   const int tid = threadIdx.x, part = tid & 31;
   const int64_t col = static_cast<int64_t>(step) * kMxStep + part * 8, row0 = group * 64 + (tid >> 5);
-  __shared__ __align__(16) unsigned char scales[kMxScaleBytes];
-  uint32_t codes[8];
-#pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const int64_t r = row0 + 8 * u < R ? row0 + 8 * u : R - 1;
-    codes[u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(packed + (r * at.steps + step) * kMxRowBytes) + part);
-  }
-  if (tid < kMxScaleBytes / 16)
-    reinterpret_cast<u32x4*>(scales)[tid] = reinterpret_cast<const u32x4*>(packed + at.codes + (group * at.steps + step) * kMxScaleBytes)[tid];
+  __shared__ __align__(16) unsigned char bytes[kMxStepBytes];
+  const u32x4* from = reinterpret_cast<const u32x4*>(packed + (group * at.steps + step) * kMxStepBytes);
+  for (int k = tid; k < kMxStepBytes / 16; k += kMxThreads) reinterpret_cast<u32x4*>(bytes)[k] = __builtin_nontemporal_load(from + k);
   __syncthreads();
   if (col >= d) return;
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
     const int64_t r = row0 + 8 * u;
     if (r >= R) break;
-    const int scale = scales[mx_scale_at((tid >> 5) + 8 * u, part >> 2)];
+    const int in_group = (tid >> 5) + 8 * u;
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(bytes + mx_code_at(in_group, part * 8));
+    const int scale = bytes[mx_scale_at(in_group, part >> 2)];
     const float unit = scale == 255 ? __builtin_nanf("") : __uint_as_float(scale == 0 ? 0x00400000u : static_cast<uint32_t>(scale) << 23);
-    const f32x2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 1);
-    const f32x2v p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u], 1.f, 3);
+    const f32x2v p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 1);
+    const f32x2v p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.f, 3);
     const float x[8] = {p0.x * unit, p0.y * unit, p1.x * unit, p1.y * unit, p2.x * unit, p2.y * unit, p3.x * unit, p3.y * unit};
     char* o = static_cast<char*>(out) + (r * ldo + col) * Elem<DT>::kBytes;
     if (col + 8 <= d) {
@@ -206,43 +204,36 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
 
 // Few rows of H: workgroup (x, y) has vocabulary rows 64 x .. + 63 and rows 16 BLOCKS y .. of H.  Its wavefronts take the steps in
 // turn and their sums are added in the LDS; the weight goes from memory to the registers of the one wavefront that needs it.
-template <int DT, int BLOCKS>
+template <int DT, int BLOCKS, bool CACHED>
 __global__ void __launch_bounds__(kMxThreads)
 fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
              void* __restrict__ out, int64_t ldo) {
   constexpr int kWaves = kMxThreads / 64;
   __shared__ __align__(16) float sums[kWaves][16 * BLOCKS][64 + 4];
-  const Mx4Layout w_at(V, d), h_at(T, d);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int steps = static_cast<int>(w_at.steps);
+  const int steps = static_cast<int>(Mx4Layout(V, d).steps);
   const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64, t0 = static_cast<int64_t>(blockIdx.y) * (16 * BLOCKS);
-  const int64_t row_bytes = w_at.steps * kMxRowBytes;
-  const unsigned char* w[4];
-  const unsigned char* h[BLOCKS];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = W + std::min<int64_t>(v0 + 16 * i + (lane & 15), V - 1) * row_bytes + (lane >> 4) * 16;
-#pragma unroll
-  for (int j = 0; j < BLOCKS; ++j) h[j] = H + std::min<int64_t>(t0 + 16 * j + (lane & 15), T - 1) * row_bytes + (lane >> 4) * 16;
-  const unsigned char* ws = W + w_at.codes + (v0 >> 6) * w_at.steps * kMxScaleBytes + lane * 8;
-  const unsigned char* hs = H + h_at.codes + (t0 >> 6) * h_at.steps * kMxScaleBytes + lane * 8;
   const int first_block = static_cast<int>((t0 >> 4) & 3);  // of H's 64 rows
+  const unsigned char* w = W + (v0 >> 6) * steps * kMxStepBytes;
+  const unsigned char* h = H + (t0 >> 6) * steps * kMxStepBytes;
   f32x4 acc[4][BLOCKS];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int s = wave; s < steps; s += kWaves) {
+    const unsigned char *ws = w + static_cast<int64_t>(s) * kMxStepBytes, *hs = h + static_cast<int64_t>(s) * kMxStepBytes;
     i32x4 a[4][2], b[BLOCKS][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) a[i][ks] = *reinterpret_cast<const i32x4*>(w[i] + s * kMxRowBytes + ks * 64);
-    const uint2 sa = *reinterpret_cast<const uint2*>(ws + static_cast<int64_t>(s) * kMxScaleBytes);
+      for (int ks = 0; ks < 2; ++ks) a[i][ks] = __builtin_bit_cast(i32x4, load_vec<CACHED>(reinterpret_cast<const u32x4*>(ws + (2 * i + ks) * kMxFragment) + lane));
+    const uint2 sa = reinterpret_cast<const uint2*>(ws + kMxCodeBytes)[lane];
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) b[j][ks] = *reinterpret_cast<const i32x4*>(h[j] + s * kMxRowBytes + ks * 64);
-    uint64_t sb = *reinterpret_cast<const uint64_t*>(hs + static_cast<int64_t>(s) * kMxScaleBytes);
+      for (int ks = 0; ks < 2; ++ks) b[j][ks] = reinterpret_cast<const i32x4*>(hs + (2 * (first_block + j) + ks) * kMxFragment)[lane];
+    uint64_t sb = reinterpret_cast<const uint64_t*>(hs + kMxCodeBytes)[lane];
     sb >>= 16 * first_block;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -279,11 +270,11 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
 }
 
 // ---- many rows of H: 256 x 256 tiles -------------------------------------------------------------------------------
-// The loop of fopd_lm_head.hip (matrix_step) on 4-bit operands: a row of a half tile is 128 bytes of a step there and here, 64
-// bf16 or 256 4-bit entries, the fragments are the same 16 bytes and the instruction takes as long, so what holds for the LDS
-// and the loads of that loop holds for this one; a product does four times the work.  The scales of a step are one more load
-// a wavefront, 512 bytes of the 64 rows that are its own to fetch (A's four groups of a tile, then B's four), requested with
-// B0 and, like B0, all read in the step's first slot:
+// The loop of fopd_lm_head.hip (matrix_step) on 4-bit operands: a half tile is 16 KB of a step there and here, 128 rows of 64 bf16 or
+// 256 4-bit entries, the fragments are the same 16 bytes a lane and the instruction takes as long; a product does four times the
+// work.  A wavefront fetches one 16-row block, two fragments, of each half tile.  The scales of a step are one more load
+// a wavefront, 512 bytes of 64 rows (the four groups of A's tile, then B's four), requested with B0 and, like B0, all
+// read in the step's first slot:
 //
 //   phase   reads              multiplies   requests                              waits for (besides its own LDS reads)
 //     1     B0, A0, scales     A0 x B0      A1 of the next step
@@ -296,29 +287,56 @@ constexpr int kMxTileLds = kLoopLdsBytes + 2 * kMxScaleLds;
 
 namespace {
 
+// One operand's half tiles: the wavefront's 16 rows of each.
+struct MxSource {
+  const unsigned char* base;
+  int groups;
+  const char* src[2];
+  __device__ __forceinline__ void locate(int r0, int steps, int wave) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      src[h] = reinterpret_cast<const char*>(base) + static_cast<int64_t>(min((r0 >> 6) + 2 * h + (wave >> 2), groups - 1)) * steps * kMxStepBytes +
+               (wave & 3) * (2 * kMxFragment);
+  }
+};
+
 struct MxLoader {
-  RowMajorSource a, b;
-  const RowMajorHalf& at;
-  uint32_t lds, scale_lds, scale_lane;
-  bool of_b;                                               // this wavefront fetches scales of B, else of A
-  const char* scales;                                      // of that matrix
-  int groups, group, steps;                                // its groups of 64 rows; place among the tile's four
+  MxSource a, b;
+  int steps, wave;
+  uint32_t lds, scale_lds;
+  uint32_t code_lane, scale_lane;                          // lane's bytes in a fragment and in the scales, from the tile's first step on
   const char* scale_src;
+  uint32_t at;                                             // bytes of the steps before this one
   __device__ __forceinline__ void locate(const GemmTile& t) {
-    a.locate(at, t.m0, 0);
-    b.locate(at, t.n0, 0);
-    scale_src = scales + static_cast<int64_t>(min(((of_b ? t.n0 : t.m0) >> 6) + group, groups - 1)) * steps * kMxScaleBytes;
+    a.locate(t.m0, steps, wave);
+    b.locate(t.n0, steps, wave);
+    const int group = wave < 4 ? min((t.m0 >> 6) + wave, a.groups - 1) : min((t.n0 >> 6) + wave - 4, b.groups - 1);
+    scale_src = reinterpret_cast<const char*>(wave < 4 ? a.base : b.base) + static_cast<int64_t>(group) * steps * kMxStepBytes + kMxCodeBytes;
+    at = 0;
   }
-  __device__ __forceinline__ void step(bool on = true) {
-    a.step(on);
-    b.step(on);
-    scale_src += on ? kMxScaleBytes : 0;
-  }
+  __device__ __forceinline__ void step(bool on = true) { at += on ? kMxStepBytes : 0; }
   __device__ __forceinline__ void request(int half, int buf) {
     const uint32_t dst = lds + buf * kStepBytes + half * kHalfBytes;
-    if (half < 2) a.request(half, dst);
-    else b.request(half - 2, dst);
-    if (half == kHalfB0) load_to_lds(scale_src, scale_lane, scale_lds + buf * kMxScaleLds);
+    const char* src = half == kHalfA0 ? a.src[0] : half == kHalfA1 ? a.src[1] : half == kHalfB0 ? b.src[0] : b.src[1];
+    load_to_lds(src, code_lane + at, dst);
+    load_to_lds(src, code_lane + at + kMxFragment, dst + kMxFragment);
+    if (half == kHalfB0) load_to_lds(scale_src, scale_lane + at, scale_lds + buf * kMxScaleLds);
+  }
+};
+
+// Where the wavefront's fragments of a step lie in the LDS.
+struct MxFragments {
+  uint32_t a_off, b_off;
+  __device__ __forceinline__ explicit MxFragments(const MatrixPlace& p) {
+    const int lane = threadIdx.x & 63;
+    a_off = p.wm * (8 * kMxFragment) + lane * 16;
+    b_off = 2 * kHalfBytes + p.wn * (4 * kMxFragment) + lane * 16;
+  }
+  __device__ __forceinline__ i32x4 a(const unsigned char* step, int half, int i, int ks) const {
+    return *reinterpret_cast<const i32x4*>(step + half * kHalfBytes + a_off + (2 * i + ks) * kMxFragment);
+  }
+  __device__ __forceinline__ i32x4 b(const unsigned char* step, int half, int j, int ks) const {
+    return *reinterpret_cast<const i32x4*>(step + half * kHalfBytes + b_off + (2 * j + ks) * kMxFragment);
   }
 };
 
@@ -344,17 +362,17 @@ __device__ __forceinline__ void mx_product(MxAcc& acc, int a, int b, const i32x4
 // STORES: stores of the tile before that are still in flight behind the requests that this step waits for (loads and stores
 // count and end in order).
 template <int STORES, typename Request>
-__device__ __forceinline__ void mx_step(MxAcc& acc, const RowMajorFragments<>& frags, const unsigned char* here, const unsigned char* scales_a,
+__device__ __forceinline__ void mx_step(MxAcc& acc, const MxFragments& frags, const unsigned char* here, const unsigned char* scales_a,
                                         const unsigned char* scales_b, Request request) {
   i32x4 fa[4][2], fb0[2][2], fb1[2][2];
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) fb0[j][ks] = __builtin_bit_cast(i32x4, frags.b(here, 0, j, ks));
+    for (int ks = 0; ks < 2; ++ks) fb0[j][ks] = frags.b(here, 0, j, ks);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) fa[i][ks] = __builtin_bit_cast(i32x4, frags.a(here, 0, i, ks));
+    for (int ks = 0; ks < 2; ++ks) fa[i][ks] = frags.a(here, 0, i, ks);
   const uint2 sa0 = *reinterpret_cast<const uint2*>(scales_a), sa1 = *reinterpret_cast<const uint2*>(scales_a + 2048);
   const uint32_t sb0 = *reinterpret_cast<const uint32_t*>(scales_b), sb1 = *reinterpret_cast<const uint32_t*>(scales_b + 2048);
   request(kHalfA1);
@@ -365,7 +383,7 @@ __device__ __forceinline__ void mx_step(MxAcc& acc, const RowMajorFragments<>& f
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) fb1[j][ks] = __builtin_bit_cast(i32x4, frags.b(here, 1, j, ks));
+    for (int ks = 0; ks < 2; ++ks) fb1[j][ks] = frags.b(here, 1, j, ks);
   request(kHalfB0);
   mx_wait<12 + STORES>();
   slot_end();
@@ -374,7 +392,7 @@ __device__ __forceinline__ void mx_step(MxAcc& acc, const RowMajorFragments<>& f
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) fa[i][ks] = __builtin_bit_cast(i32x4, frags.a(here, 1, i, ks));
+    for (int ks = 0; ks < 2; ++ks) fa[i][ks] = frags.a(here, 1, i, ks);
   request(kHalfA0);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   slot_end();
@@ -471,27 +489,19 @@ __global__ void __launch_bounds__(kLmThreads)
 fopd_mx4_tiles(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
                void* __restrict__ out, int64_t ldo, int tiles_m, int tiles_n) {
   extern __shared__ __align__(16) unsigned char mx_smem[];
-  const Mx4Layout w_at(V, d), h_at(T, d);
-  const int steps = static_cast<int>(w_at.steps);
+  const int steps = static_cast<int>(Mx4Layout(V, d).steps);
   TileWalk<true, WALK> walk = {tiles_m, tiles_n, steps, 1};
   GemmTile tile;
   if (!walk.first(tile, blockIdx.x)) return;               // whole workgroup, before any barrier
 
   const MatrixPlace mine = matrix_place(mx_smem);
-  const RowMajorHalf at(mine);
-  const RowMajorFragments<> frags(mine);
+  const MxFragments frags(mine);
   const int lane = threadIdx.x & 63, wave = mine.wm * 4 + mine.wn;
   const unsigned char* scales = mx_smem + kLoopLdsBytes;
   const unsigned char* scales_a = scales + mine.wm * 1024 + lane * 8;
   const unsigned char* scales_b = scales + (4 + (mine.wn >> 1)) * 1024 + lane * 8 + (mine.wn & 1) * 4;
-  MxLoader load = {{}, {}, at, mine.lds, mine.lds - wave * 2048u + kLoopLdsBytes + wave * 1024u, (lane & 31) * 16u,
-                   wave >= 4, reinterpret_cast<const char*>(wave >= 4 ? H + h_at.codes : W + w_at.codes),
-                   static_cast<int>(wave >= 4 ? h_at.groups : w_at.groups), wave & 3, steps, nullptr};
-  load.a.base = reinterpret_cast<const char*>(W);
-  load.a.ld = load.b.ld = w_at.steps * (kMxRowBytes / 2);  // (the source counts in 2-byte entries)
-  load.a.rows = static_cast<int>(V);
-  load.b.base = reinterpret_cast<const char*>(H);
-  load.b.rows = static_cast<int>(T);
+  MxLoader load = {{W, static_cast<int>((V + 63) >> 6), {}}, {H, static_cast<int>((T + 63) >> 6), {}}, steps, wave, mine.lds,
+                   mine.lds - wave * 2048u + kLoopLdsBytes + wave * 1024u, lane * 16u, (lane & 31) * 16u, nullptr, 0};
 
   // the stream of steps, as matrix_tiles
   constexpr int kStores = DT == FOPD_F32 ? 32 : 16;        // of a whole tile, by a wavefront

@@ -11,12 +11,12 @@ P = ctypes.c_void_p
 
 
 def test_mx4_sizes():
-    # codes: 128 bytes a row and 256 entries, rounded up to 256; scales: 512 bytes for 64 rows and 256 entries
-    assert fb.fopd_mx4_bytes(1, 1) == 256 + 512
-    assert fb.fopd_mx4_bytes(2, 256) == 256 + 512
-    assert fb.fopd_mx4_bytes(65, 257) == 65 * 256 + 2 * 2 * 512
+    # 64 rows and 256 entries: 8192 bytes of codes, 512 of scales
+    assert fb.fopd_mx4_bytes(1, 1) == 8704
+    assert fb.fopd_mx4_bytes(64, 256) == 8704
+    assert fb.fopd_mx4_bytes(65, 257) == 4 * 8704
     assert fb.fopd_mx4_bytes(0, 64) == 0
-    assert fb.fopd_mx4_bytes(151936, 4096) == 151936 * 2048 + 2374 * 16 * 512
+    assert fb.fopd_mx4_bytes(151936, 4096) == 2374 * 16 * 8704
     assert fb.fopd_mx4_logits_workspace_bytes(45, 151936, 4096) >= 256 + fb.fopd_mx4_bytes(45, 4096)
 
 
@@ -34,6 +34,7 @@ def test_mx4_rejects_bad_arguments_before_launch():
         assert call(packed=8192 + 8) == 3
         assert call(R=-1) == 2
         assert call(d=0) == 2
+        assert call(d=(1 << 24) + 8, **{"ld" if call is quantize else "ldo": 1 << 25}) == 2
         assert call(dt=2) == 4
         assert call(n=fb.fopd_mx4_bytes(8, 64) - 1) == 5
         assert call(R=0) == 0
