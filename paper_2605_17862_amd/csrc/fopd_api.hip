@@ -679,14 +679,24 @@ fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d,
 }
 
 // A weight that fits the Infinity Cache with something to spare is read by ordinary loads and may still be there for the next
-// token; a larger one is read past it.  One row, d = 4096, ordinary / non-temporal: 32,000 entries 17.9 / 19.8 us, 151,936 69 / 55 us (the
-// codes row by row).
-constexpr int64_t kMxCachedBytes = 192LL << 20;
+// token; a larger one is read past it.  16 rows, d = 4096, call after call, ordinary / non-temporal: 4096 entries (8 rows) 10.8 / 14.7 us,
+// 32,000 16.1 / 19.6, 70,000 (two weights in turn, 305 MB) 34.1 / 31.0, 100,000 47.0 / 41.3; one row x 151,936 61.2 / 54.1.
+constexpr int64_t kMxCachedBytes = 128LL << 20;
+constexpr int64_t kMxFewRows = 64;
+
+// launch(type, whether the weight is read by ordinary loads), both as types.
+template <typename Launch>
+fopd_status mx4_variant(fopd_dtype dt, bool cached, Launch launch) {
+  typedef std::integral_constant<int, FOPD_BF16> B16;
+  typedef std::integral_constant<int, FOPD_F32> F32;
+  if (dt == FOPD_BF16) return cached ? launch(B16(), std::true_type()) : launch(B16(), std::false_type());
+  return cached ? launch(F32(), std::true_type()) : launch(F32(), std::false_type());
+}
 
 // weight [V, d] and hidden rows [T, d], both packed.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
-  if (T > 64) {
+  if (T > kMxFewRows) {
     const int tiles_m = static_cast<int>((V + kGemmTile - 1) / kGemmTile), tiles_n = static_cast<int>((T + kGemmTile - 1) / kGemmTile);
     const bool walk = gemm_walks(static_cast<int64_t>(tiles_m) * tiles_n, Mx4Layout(V, d).steps, false);
     auto tiles = dt == FOPD_BF16 ? (walk ? fopd_mx4_tiles<FOPD_BF16, true> : fopd_mx4_tiles<FOPD_BF16, false>)
@@ -697,19 +707,15 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
     tiles<<<gemm_grid((tile_groups(tiles_m, tiles_n) + 7) / 8, walk), kLmThreads, kMxTileLds, s>>>(w, V, h, T, d, out, ldo, tiles_m, tiles_n);
     return launched();
   }
-  const int blocks = T <= 16 ? 1 : (T <= 32 ? 2 : 4);
-  const dim3 grid(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((T + 16 * blocks - 1) / (16 * blocks)));
-  auto launch = [&](auto dt_tag, auto cached_tag) {
+  const int blocks = static_cast<int>(T + 15) / 16;
+  return mx4_variant(dt, Mx4Layout(V, d).total <= kMxCachedBytes, [&](auto dt_tag, auto cached_tag) {
     constexpr int DT = decltype(dt_tag)::value;
     constexpr bool CACHED = decltype(cached_tag)::value;
-    auto kern = blocks == 1 ? fopd_mx4_few<DT, 1, CACHED> : blocks == 2 ? fopd_mx4_few<DT, 2, CACHED> : fopd_mx4_few<DT, 4, CACHED>;
-    kern<<<grid, kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
+    auto kern = blocks == 1 ? fopd_mx4_few<DT, 1, CACHED> : blocks == 2 ? fopd_mx4_few<DT, 2, CACHED>
+                : blocks == 3 ? fopd_mx4_few<DT, 3, CACHED> : fopd_mx4_few<DT, 4, CACHED>;
+    kern<<<static_cast<unsigned>((V + 63) / 64), kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
     return launched();
-  };
-  typedef std::integral_constant<int, FOPD_BF16> B16;
-  typedef std::integral_constant<int, FOPD_F32> F32;
-  if (Mx4Layout(V, d).total <= kMxCachedBytes) return dt == FOPD_BF16 ? launch(B16(), std::true_type()) : launch(F32(), std::true_type());
-  return dt == FOPD_BF16 ? launch(B16(), std::false_type()) : launch(F32(), std::false_type());
+  });
 }
 
 // ---- verification of drafted tokens ---------------------------------------------------------

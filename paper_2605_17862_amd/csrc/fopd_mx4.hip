@@ -202,27 +202,29 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
   }
 }
 
-// Few rows of H: workgroup (x, y) has vocabulary rows 64 x .. + 63 and rows 16 BLOCKS y .. of H.  Its wavefronts take the steps in
-// turn and their sums are added in the LDS; the weight goes from memory to the registers of the one wavefront that needs it.
+// Up to 64 rows of H: workgroup x has vocabulary rows 64 x .. + 63.  Its wavefronts take the steps in turn and their sums are added
+// in the LDS; the weight goes from memory to the registers of the one wavefront that needs it.  Bound by HBM: one row 48 us = 6.8
+// TB/s; with results to write the rate falls to that of mixed traffic, 45 rows (14 MB of bf16) 65 us = 5.3 TB/s.  Results of 49 - 64
+// rows past the caches: 80 -> 74.5 us, of fewer no faster (30 rows 63.8 / 65.1).  (H in the LDS of one workgroup a compute unit, whose
+// wavefronts stream sixteen vocabulary rows each: 1 / 45 / 64 rows 58.6 / 72 / 76 us where this takes 54 / 70 / 75; eight
+// wavefronts a workgroup: 95 for one row, with the codes row by row, where four took 69.)
 template <int DT, int BLOCKS, bool CACHED>
 __global__ void __launch_bounds__(kMxThreads)
 fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
              void* __restrict__ out, int64_t ldo) {
   constexpr int kWaves = kMxThreads / 64;
-  __shared__ __align__(16) float sums[kWaves][16 * BLOCKS][64 + 4];
+  __shared__ __align__(16) float sums[kWaves / 2][16 * BLOCKS][64 + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int steps = static_cast<int>(Mx4Layout(V, d).steps);
-  const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64, t0 = static_cast<int64_t>(blockIdx.y) * (16 * BLOCKS);
-  const int first_block = static_cast<int>((t0 >> 4) & 3);  // of H's 64 rows
+  const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64;
   const unsigned char* w = W + (v0 >> 6) * steps * kMxStepBytes;
-  const unsigned char* h = H + (t0 >> 6) * steps * kMxStepBytes;
   f32x4 acc[4][BLOCKS];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int s = wave; s < steps; s += kWaves) {
-    const unsigned char *ws = w + static_cast<int64_t>(s) * kMxStepBytes, *hs = h + static_cast<int64_t>(s) * kMxStepBytes;
+    const unsigned char *ws = w + static_cast<int64_t>(s) * kMxStepBytes, *hs = H + static_cast<int64_t>(s) * kMxStepBytes;
     i32x4 a[4][2], b[BLOCKS][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -232,9 +234,8 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) b[j][ks] = reinterpret_cast<const i32x4*>(hs + (2 * (first_block + j) + ks) * kMxFragment)[lane];
-    uint64_t sb = reinterpret_cast<const uint64_t*>(hs + kMxCodeBytes)[lane];
-    sb >>= 16 * first_block;
+      for (int ks = 0; ks < 2; ++ks) b[j][ks] = reinterpret_cast<const i32x4*>(hs + (2 * j + ks) * kMxFragment)[lane];
+    const uint64_t sb = reinterpret_cast<const uint64_t*>(hs + kMxCodeBytes)[lane];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -245,22 +246,38 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
                                   static_cast<int>(j < 2 ? sb : sb >> 32), 2 * (j & 1) + ks);
   }
   // register r of acc[i][j]: vocabulary row 16 i + 4 (lane / 16) + r, row 16 j + lane % 16 of H
+  // (the upper half of the wavefronts hands its sums to the lower one)
+  auto place = [&](int i, int j) { return reinterpret_cast<f32x4*>(&sums[wave & (kWaves / 2 - 1)][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4)]); };
+  if (wave >= kWaves / 2) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < BLOCKS; ++j)
-      *reinterpret_cast<f32x4*>(&sums[wave][16 * j + (lane & 15)][16 * i + 4 * (lane >> 4)]) = acc[i][j];
+      for (int j = 0; j < BLOCKS; ++j) *place(i, j) = acc[i][j];
+  }
+  __syncthreads();
+  if (wave < kWaves / 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < BLOCKS; ++j) *place(i, j) += acc[i][j];
+  }
   __syncthreads();
   for (int k = tid; k < 16 * BLOCKS * 16; k += kMxThreads) {            // four neighbouring results each
     const int t = k >> 4, v = 4 * (k & 15);
     f32x4 z = *reinterpret_cast<const f32x4*>(&sums[0][t][v]);
 #pragma unroll
-    for (int u = 1; u < kWaves; ++u) z += *reinterpret_cast<const f32x4*>(&sums[u][t][v]);
-    if (t0 + t >= T || v0 + v >= V) continue;
-    char* o = static_cast<char*>(out) + ((t0 + t) * ldo + v0 + v) * Elem<DT>::kBytes;
+    for (int u = 1; u < kWaves / 2; ++u) z += *reinterpret_cast<const f32x4*>(&sums[u][t][v]);
+    if (t >= T || v0 + v >= V) continue;
+    char* o = static_cast<char*>(out) + (t * ldo + v0 + v) * Elem<DT>::kBytes;
     if (v0 + v + 4 <= V) {
-      if constexpr (DT == FOPD_BF16) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]));
-      else *reinterpret_cast<f32x4*>(o) = z;
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      u32x2* o16 = reinterpret_cast<u32x2*>(o);
+      f32x4* o32 = reinterpret_cast<f32x4*>(o);
+      const u32x2 z16 = {pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+      if constexpr (DT == FOPD_BF16 && BLOCKS < 4) *o16 = z16;
+      else if constexpr (DT == FOPD_BF16) __builtin_nontemporal_store(z16, o16);
+      else if constexpr (BLOCKS < 4) *o32 = z;
+      else __builtin_nontemporal_store(z, o32);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
