@@ -659,7 +659,7 @@ fopd_status check_mx4(const void* packed, size_t bytes, int64_t R, int64_t d) {
   return FOPD_OK;
 }
 
-// launch(first group of 64 rows, groups): a workgroup of 256 lanes for each group and step.
+// launch(first group of 64 rows, workgroups): one for each group and step.
 template <typename Launch>
 fopd_status mx4_in_slabs(const Mx4Layout& at, Launch launch) {
   const int64_t most = std::max<int64_t>(1, (1LL << 22) / at.steps);
@@ -674,7 +674,7 @@ fopd_status mx4_in_slabs(const Mx4Layout& at, Launch launch) {
 fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed, hipStream_t s) {
   auto kern = dt == FOPD_BF16 ? fopd_mx4_pack<FOPD_BF16> : fopd_mx4_pack<FOPD_F32>;
   return mx4_in_slabs(Mx4Layout(R, d), [&](int64_t g, unsigned n) {
-    kern<<<n, kMxThreads, 0, s>>>(in, ld, R, d, static_cast<unsigned char*>(packed), g);
+    kern<<<n, kMxPackThreads, 0, s>>>(in, ld, R, d, static_cast<unsigned char*>(packed), g);
   });
 }
 
@@ -1975,7 +1975,7 @@ fopd_status fopd_mx4_dequantize(const void* packed, size_t packed_bytes, int64_t
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto kern = dt == FOPD_BF16 ? fopd_mx4_unpack<FOPD_BF16> : fopd_mx4_unpack<FOPD_F32>;
   return mx4_in_slabs(Mx4Layout(R, d), [&](int64_t g, unsigned n) {
-    kern<<<n, kMxThreads, 0, s>>>(static_cast<const unsigned char*>(packed), R, d, out, ldo, g);
+    kern<<<n, kMxPackThreads, 0, s>>>(static_cast<const unsigned char*>(packed), R, d, out, ldo, g);
   });
 }
 

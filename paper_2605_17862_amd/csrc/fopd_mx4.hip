@@ -40,6 +40,7 @@ constexpr int kMxCodeBytes = 8192;            // of 64 rows and a step
 constexpr int kMxScaleBytes = 512;
 constexpr int kMxStepBytes = kMxCodeBytes + kMxScaleBytes;
 constexpr int kMxThreads = 256;
+constexpr int kMxPackThreads = 512;          // of the two kernels that change the order
 constexpr int64_t kMxMaxEntries = 1 << 24;     // of a row: its packed bytes are counted in 32 bits
 
 struct Mx4Layout {
@@ -91,12 +92,13 @@ __device__ __forceinline__ f32x4 mx_multiply(const i32x4& a, const i32x4& b, con
 
 }  // namespace
 
-// Workgroup (group - first_group) x steps + step: 64 rows of one step, sixteen a wavefront.  A block is 32 / E neighbouring lanes of E entries.
+// Workgroup (group - first_group) x steps + step: 64 rows of one step.  A block is 32 / E neighbouring lanes of E entries.
 // Columns d and on are zeros and are not read; so are rows past the last.
 template <int DT>
-__global__ void __launch_bounds__(kMxThreads)
+__global__ void __launch_bounds__(kMxPackThreads)
 fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, unsigned char* __restrict__ packed, int64_t first_group) {
   constexpr int E = Elem<DT>::kPerVec, kLanesPerRow = kMxStep / E, kRows = 64 / kLanesPerRow;   // rows of a wavefront at a time
+  constexpr int kWaveRows = 64 * 64 / kMxPackThreads;
   const Mx4Layout at(R, d);
   const unsigned steps = static_cast<unsigned>(at.steps), in_launch = blockIdx.x / steps;
   const int64_t group = first_group + in_launch;
@@ -105,10 +107,10 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
   const int part = lane % kLanesPerRow;                    // of a row's step
   const int64_t col = static_cast<int64_t>(step) * kMxStep + part * E;
   __shared__ __align__(16) unsigned char bytes[kMxStepBytes];
-  const int row0 = wave * 16 + lane / kLanesPerRow;
-  u32x4 q[16 / kRows];
+  const int row0 = wave * kWaveRows + lane / kLanesPerRow;
+  u32x4 q[kWaveRows / kRows];
 #pragma unroll
-  for (int u = 0; u < 16 / kRows; ++u) {
+  for (int u = 0; u < kWaveRows / kRows; ++u) {
     const int64_t r = group * 64 + row0 + u * kRows;
     q[u] = u32x4{0u, 0u, 0u, 0u};
     if (r >= R || col >= d) continue;
@@ -123,7 +125,7 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
     }
   }
 #pragma unroll
-  for (int u = 0; u < 16 / kRows; ++u) {
+  for (int u = 0; u < kWaveRows / kRows; ++u) {
     const int in_group = row0 + u * kRows;
     float x[E];
     unpack<DT>(q[u], x);
@@ -154,12 +156,12 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
   }
   __syncthreads();
   u32x4* out = reinterpret_cast<u32x4*>(packed + (group * at.steps + step) * kMxStepBytes);
-  for (int k = tid; k < kMxStepBytes / 16; k += kMxThreads) __builtin_nontemporal_store(reinterpret_cast<const u32x4*>(bytes)[k], out + k);
+  for (int k = tid; k < kMxStepBytes / 16; k += kMxPackThreads) __builtin_nontemporal_store(reinterpret_cast<const u32x4*>(bytes)[k], out + k);
 }
 
 // Workgroup (group - first_group) x steps + step, eight entries a lane.
 template <int DT>
-__global__ void __launch_bounds__(kMxThreads)
+__global__ void __launch_bounds__(kMxPackThreads)
 fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, void* __restrict__ out, int64_t ldo,
                 int64_t first_group) {
   typedef float f32x2v __attribute__((ext_vector_type(2)));
@@ -171,14 +173,14 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
   const int64_t col = static_cast<int64_t>(step) * kMxStep + part * 8, row0 = group * 64 + (tid >> 5);
   __shared__ __align__(16) unsigned char bytes[kMxStepBytes];
   const u32x4* from = reinterpret_cast<const u32x4*>(packed + (group * at.steps + step) * kMxStepBytes);
-  for (int k = tid; k < kMxStepBytes / 16; k += kMxThreads) reinterpret_cast<u32x4*>(bytes)[k] = __builtin_nontemporal_load(from + k);
+  for (int k = tid; k < kMxStepBytes / 16; k += kMxPackThreads) reinterpret_cast<u32x4*>(bytes)[k] = __builtin_nontemporal_load(from + k);
   __syncthreads();
   if (col >= d) return;
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const int64_t r = row0 + 8 * u;
+  for (int u = 0; u < 64 * 32 / kMxPackThreads; ++u) {
+    const int64_t r = row0 + (kMxPackThreads / 32) * u;
     if (r >= R) break;
-    const int in_group = (tid >> 5) + 8 * u;
+    const int in_group = (tid >> 5) + (kMxPackThreads / 32) * u;
     const uint32_t codes = *reinterpret_cast<const uint32_t*>(bytes + mx_code_at(in_group, part * 8));
     const int scale = bytes[mx_scale_at(in_group, part >> 2)];
     const float unit = scale == 255 ? __builtin_nanf("") : __uint_as_float(scale == 0 ? 0x00400000u : static_cast<uint32_t>(scale) << 23);
