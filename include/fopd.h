@@ -693,7 +693,7 @@ fopd_status fopd_verify_draft(const void* target_logits, const void* draft_logit
  * the element type is needed (16 bytes are faster).  out == grad (then of the same type and pitch) clips in place; else
  * no memory may be shared.  rows or cols of 0 are allowed, and so is n = 0 (sum 0).  fopd_grad_norm does not use out.
  * `tensors_host` is HOST memory, read before the call returns; the pointers in it are device pointers.
- *   workspace of fopd_grad_norm: fopd_grad_workspace_bytes() bytes, 256-byte aligned; nothing in it has to be initialised
+ *   workspace of fopd_grad_norm: fopd_grad_workspace_bytes() bytes, 256-byte aligned, initialised once with fopd_workspace_init
  */
 typedef struct {
   const void* grad;

@@ -758,8 +758,11 @@ fopd_status launch_verify(const VerifyArgs& a, const VerifyPlan& plan, void* ws,
 
 // ---- gradient norm and clipping ------------------------------------------------------------
 
-constexpr int kGradPartials = 1 << 16;
-constexpr int kGradGrid = 2048;                           // workgroups of a launch: eight a compute unit
+constexpr int kGradPartials = 1 << 14;
+// Workgroups of a launch.  The norm's draw a ticket each, one after the other: 2 / 4 / 8 a compute unit, 32,000 x 1000 fp32 64.8 /
+// 68.5 / 75.6 us, 151,936 x 4096 1243 / 1245 / 1253; 1 a compute unit 69 and 1360.  The scaling of 622 M entries wants more than
+// two (4 / 8 / 16: + 0.5 % / 0 / - 1 %; of 32 M entries 64.4 / 66.0 / 69.2 us).
+constexpr int kGradSumGrid = 512, kGradScaleGrid = 2048;
 
 fopd_status check_grad_tensor(const fopd_grad_tensor& t, bool with_out) {
   if ((t.dt != FOPD_F32 && t.dt != FOPD_BF16) || (with_out && t.dt_out != FOPD_F32 && t.dt_out != FOPD_BF16)) return FOPD_EDTYPE;
@@ -2047,28 +2050,32 @@ fopd_status fopd_grad_norm(const fopd_grad_tensor* tensors_host, int32_t n, int 
   hipStream_t s = static_cast<hipStream_t>(stream);
   double* partial = at<double>(workspace, 256);
   int used = 0;
-  bool add = accumulate != 0;
-  auto finish = [&](float* to) {
-    fopd_grad_norm_final<<<1, kGradLanes, 0, s>>>(partial, used, add, sum_sq, to);
-    used = 0;
-    add = true;
-    return launched();
-  };
   int64_t pieces = 0;                                      // of the tables to come
   for (int32_t i = 0; i < n; ++i) pieces += tensors_host[i].rows * tensors_host[i].cols / (kGradPieceBytes >> (tensors_host[i].dt == FOPD_BF16 ? 1 : 2));
-  const fopd_status st = grad_tables(tensors_host, n, false, [&](const GradTable& g) {
+  GradFinish finish = {0, accumulate != 0, sum_sq, norm, at<int32_t>(workspace, 0) + 1};
+  // (a table is launched when the next one is there, so that the last launch is known as such)
+  GradTable waiting;
+  waiting.n = waiting.pieces = 0;
+  auto launch = [&](const GradTable& g, bool last) {
+    const int grid = std::max(1, std::min(g.pieces, kGradSumGrid));
     const int64_t first_cached = std::min<int64_t>(std::max<int64_t>(0, pieces - (200LL << 20) / kGradPieceBytes), g.pieces);
     pieces -= g.pieces;
-    const int grid = std::min(g.pieces, kGradGrid);
-    if (used + grid > kGradPartials) {
-      const fopd_status full = finish(nullptr);
-      if (full != FOPD_OK) return full;
-    }
-    fopd_grad_sum_squares<<<static_cast<unsigned>(grid), kGradLanes, 0, s>>>(g, partial + used, static_cast<int>(first_cached));
+    finish.norm = last ? norm : nullptr;
+    finish.count = last || used + grid + kGradSumGrid > kGradPartials ? used + grid : 0;
+    fopd_grad_sum_squares<<<static_cast<unsigned>(grid), kGradLanes, 0, s>>>(g, partial + used, static_cast<int>(first_cached), finish);
     used += grid;
+    if (finish.count > 0) {                                // no room for another launch: the sum so far goes into sum_sq
+      finish.add = true;
+      used = 0;
+    }
     return launched();
+  };
+  const fopd_status st = grad_tables(tensors_host, n, false, [&](const GradTable& g) {
+    const fopd_status before = waiting.n > 0 ? launch(waiting, false) : FOPD_OK;
+    waiting = g;
+    return before;
   });
-  return st != FOPD_OK ? st : finish(norm);
+  return st != FOPD_OK ? st : launch(waiting, true);
 }
 
 fopd_status fopd_grad_clip(const fopd_grad_tensor* tensors_host, int32_t n, const double* sum_sq, float max_norm, float eps,
@@ -2085,7 +2092,7 @@ fopd_status fopd_grad_clip(const fopd_grad_tensor* tensors_host, int32_t n, cons
     coef = nullptr;                                        // (written by the first launch)
     return launched();
   };
-  const fopd_status st = grad_tables(tensors_host, n, true, [&](const GradTable& g) { return scale(g, std::min(g.pieces, kGradGrid)); });
+  const fopd_status st = grad_tables(tensors_host, n, true, [&](const GradTable& g) { return scale(g, std::min(g.pieces, kGradScaleGrid)); });
   if (st != FOPD_OK || coef == nullptr) return st;
   GradTable none;
   none.n = none.pieces = 0;

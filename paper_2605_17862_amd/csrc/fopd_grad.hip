@@ -1,7 +1,7 @@
 // Global norm of a list of gradient tensors and their scaling by it, for gfx950 (CDNA4).
 //
-//   fopd_grad_sum_squares   sum of squares of a workgroup's pieces of the list, in 64 bits
-//   fopd_grad_norm_final    the workgroups' sums in their order: sum of squares and norm
+//   fopd_grad_sum_squares   sum of squares of a workgroup's pieces of the list, in 64 bits; the last workgroup of a list's last launch
+//                           adds the workgroups' sums up, in their order: sum of squares and norm
 //   fopd_grad_scale         out = c grad,  c = min(1, max_norm / (norm + eps))
 //
 // Bound by HBM: the norm reads the list once, the scaling reads it and writes it.  Squares are formed and added in 64 bits, at
@@ -28,7 +28,6 @@ constexpr int kGradTable = 48;
 constexpr int kGradPieceBytes = 32768;
 constexpr int kGradLanes = 256;
 constexpr int kGradVecs = kGradPieceBytes / 16 / kGradLanes;
-constexpr int kGradMaxGroups = 4096;          // workgroups of a launch of fopd_grad_sum_squares
 constexpr int64_t kGradMaxPieces = 1LL << 30; // pieces of a launch
 
 struct GradEntry {
@@ -149,9 +148,18 @@ __device__ __forceinline__ void grad_piece_scale(const char* p, char* o, int cou
 
 }  // namespace
 
-// Pieces from first_cached on stay in the Infinity Cache.
+// What the last launch of a list leaves behind: the root and sum of `count` partial sums (of earlier launches too).
+struct GradFinish {
+  int count;                                  // 0: not the last launch
+  bool add;                                   // to what sum_sq holds
+  double* sum_sq;
+  float* norm;                                // may be NULL
+  int32_t* ticket;                            // 0 before and after
+};
+
+// Pieces from first_cached on stay in the Infinity Cache.  partial: this launch's first.
 __global__ void __launch_bounds__(kGradLanes)
-fopd_grad_sum_squares(GradTable g, double* __restrict__ partial, int first_cached) {
+fopd_grad_sum_squares(GradTable g, double* partial, int first_cached, GradFinish finish) {
   double sum = 0.0;
   for (int piece = blockIdx.x; piece < g.pieces; piece += gridDim.x) {
     const GradEntry& t = g.t[grad_tensor_of(g, piece)];
@@ -162,21 +170,26 @@ fopd_grad_sum_squares(GradTable g, double* __restrict__ partial, int first_cache
     else sum += t.bf16 ? grad_piece_squares<FOPD_BF16, false>(p, at.count) : grad_piece_squares<FOPD_F32, false>(p, at.count);
   }
   __shared__ double sh[kGradLanes / 64];
+  __shared__ int last;
   sum = block_sum<kGradLanes>(sum, sh);
-  if (threadIdx.x == 0) partial[blockIdx.x] = sum;
-}
-
-// sum_sq = (add: sum_sq +) the n partial sums; norm (last launch of a list, else NULL) = its root.
-__global__ void __launch_bounds__(kGradLanes)
-fopd_grad_norm_final(const double* __restrict__ partial, int n, bool add, double* __restrict__ sum_sq, float* __restrict__ norm) {
-  double sum = 0.0;
-  for (int k = threadIdx.x; k < n; k += kGradLanes) sum += partial[k];
-  __shared__ double sh[kGradLanes / 64];
+  if (threadIdx.x == 0) {
+    // The sum goes to where all XCDs' caches meet, and is there before the ticket is drawn: whoever draws the last ticket finds
+    // them all.  (Which workgroup that is does not matter, the order of the additions is that of the list.)
+    __hip_atomic_store(partial + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = finish.count > 0 && __hip_atomic_fetch_add(finish.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<int>(gridDim.x) - 1;
+  }
+  __syncthreads();
+  if (last == 0) return;
+  const double* from = partial + gridDim.x - finish.count;
+  sum = 0.0;
+  for (int k = threadIdx.x; k < finish.count; k += kGradLanes) sum += __hip_atomic_load(from + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   sum = block_sum<kGradLanes>(sum, sh);
   if (threadIdx.x != 0) return;
-  if (add) sum += sum_sq[0];
-  sum_sq[0] = sum;
-  if (norm != nullptr) norm[0] = static_cast<float>(sqrt(sum));
+  if (finish.add) sum += finish.sum_sq[0];
+  finish.sum_sq[0] = sum;
+  if (finish.norm != nullptr) finish.norm[0] = static_cast<float>(sqrt(sum));
+  *finish.ticket = 0;
 }
 
 // c < 1 or NaN as it is, else 1: a norm that is no number makes every entry one.

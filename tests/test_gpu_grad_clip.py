@@ -16,9 +16,11 @@ EPS = 1e-6
 
 def _ws():
     n = fb.fopd_grad_workspace_bytes()
-    ws = torch.full((n + 256,), 255, dtype=torch.uint8, device=DEV)          # nothing in it has to be initialised
+    ws = torch.full((n + 256,), 255, dtype=torch.uint8, device=DEV)
     off = (-ws.data_ptr()) % 256
-    return ws[off:off + n]
+    ws = ws[off:off + n]
+    fb.fopd_workspace_init(ws)
+    return ws
 
 
 def _scalars():
@@ -48,8 +50,9 @@ def _check(grads, outs, before, max_norm, sum_sq, norm, coef):
         assert (np.abs(_f64(o) - w) <= tol).all()
 
 
+# (no tensor at all, one table, its last entry, more tables than one, more than one table with empty tensors between)
 SHAPES = [[(1,)], [(7,), (8,), (0,), (9, 0), (3, 5)], [(8191,), (8192,), (8193,)], [(300, 500), (16385,), (2, 3, 70)],
-          [(1000, 1000)] + 60 * [(33,)], 130 * [(257,)]]
+          [(1000, 1000)] + 60 * [(33,)], 130 * [(257,)], 48 * [(3,)], 49 * [(3,), (0,)]]
 
 
 @pytest.mark.parametrize("shapes", SHAPES)
@@ -148,6 +151,20 @@ def test_lists_in_parts_add_up():
     fb.fopd_grad_norm(fb.grad_tensors(grads[:1]), parts, None, ws)
     fb.fopd_grad_norm(fb.grad_tensors(grads[1:]), parts, norm_parts, ws, accumulate=True)
     assert float(parts) == pytest.approx(float(sum_sq), rel=1e-13) and float(norm_parts) == pytest.approx(float(norm), rel=1e-7)
+
+
+def test_more_tensors_than_the_workspace_has_sums_for():
+    """50 tables of 48 tensors, each with more pieces than a launch has workgroups: sums are folded on the way."""
+    piece = 8192
+    one = torch.ones(50 * piece, device=DEV)
+    tensors = fb.grad_tensors(50 * 48 * [one])
+    sum_sq, norm, _ = _scalars()
+    ws = _ws()
+    for _ in range(2):
+        fb.fopd_grad_norm(tensors, sum_sq, norm, ws)
+        assert float(sum_sq) == 50 * 48 * 50 * piece                         # (whole numbers: exact)
+    fb.fopd_grad_norm(tensors, sum_sq, norm, ws, accumulate=True)
+    assert float(sum_sq) == 2 * 50 * 48 * 50 * piece
 
 
 def test_same_bits_each_time_and_in_a_captured_graph():
