@@ -618,6 +618,7 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
  *                      once.  fp32 sums, rounded once to `dt`; columns V .. ld - 1 of the logits are not written.  What a
  *                      drafter runs for each token it proposes (fopd_verify_draft takes its logits), or a scoring pass
  *                      whose teacher or policy is served with such a projection.
+ *                      V at most 2^28.
  *   workspace          fopd_mx4_logits_workspace_bytes(T, V, d) bytes, 256-byte aligned; nothing in it has to be initialised
  * The sum over k of a result is taken in an order that goes by T, V and d, not by its place: the same hidden row in a call of
  * another T may differ in its last bits.  The first call in a process sets a kernel attribute: make one call before
@@ -662,7 +663,7 @@ fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ld
  *   n_accepted     [B] int32 out
  *   out_ids, out_logp, out_mask   [R] int32, f32, uint8 out: rows 0 .. a of a sample get the token, log p_j(token) and 1, its
  *                  rows behind -1, 0 and 0 (up to max_draft in a padded batch): token_ids, behav_logp and mask of the loss.
- *                  Rows of no sample stay as they were.  Samples must not share rows.
+ *                  Rows of no sample stay as they were.  Samples must not share rows, nor outputs memory with inputs.
  *   workspace      fopd_verify_workspace_bytes(R, V, B) bytes, 256-byte aligned, initialised once with fopd_workspace_init
  *
  * On the device: draft_lens outside 0 .. max_draft or rows outside [0, R) raise FOPD_ESEGMENTS, n_accepted is 0 and no row is
@@ -691,7 +692,7 @@ fopd_status fopd_verify_draft(const void* target_logits, const void* draft_logit
  *                  A norm that is NaN or infinite makes c NaN or 0, and the results accordingly.
  * A tensor is `rows` rows of `cols` entries, row r at grad + r ld; out likewise with ld_out, of the same shape.  Only the alignment of
  * the element type is needed (16 bytes are faster).  out == grad (then of the same type and pitch) clips in place; else
- * no memory may be shared.  rows or cols of 0 are allowed, and so is n = 0 (sum 0).  fopd_grad_norm does not use out.
+ * no memory may be shared.  A tensor has at most 2^40 entries; rows or cols of 0 are allowed, and so is n = 0 (sum 0).  fopd_grad_norm does not use out.
  * `tensors_host` is HOST memory, read before the call returns; the pointers in it are device pointers.
  *   workspace of fopd_grad_norm: fopd_grad_workspace_bytes() bytes, 256-byte aligned, initialised once with fopd_workspace_init
  */

@@ -683,6 +683,7 @@ fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d,
 // 32,000 16.1 / 19.6, 70,000 (two weights in turn, 305 MB) 34.1 / 31.0, 100,000 47.0 / 41.3; one row x 151,936 61.2 / 54.1.
 constexpr int64_t kMxCachedBytes = 128LL << 20;
 constexpr int64_t kMxFewRows = 64;
+constexpr int64_t kMxMaxVocabulary = 1LL << 28;           // (a launch has at most 2^32 lanes)
 
 // launch(type, whether the weight is read by ordinary loads), both as types.
 template <typename Launch>
@@ -767,8 +768,9 @@ constexpr int kGradSumGrid = 512, kGradScaleGrid = 2048;
 fopd_status check_grad_tensor(const fopd_grad_tensor& t, bool with_out) {
   if ((t.dt != FOPD_F32 && t.dt != FOPD_BF16) || (with_out && t.dt_out != FOPD_F32 && t.dt_out != FOPD_BF16)) return FOPD_EDTYPE;
   constexpr int64_t kMost = 1LL << 40;
-  if (t.rows < 0 || t.cols < 0 || t.rows > kMost || t.cols > kMost) return FOPD_ESHAPE;
+  if (t.rows < 0 || t.cols < 0) return FOPD_ESHAPE;
   if (t.rows == 0 || t.cols == 0) return FOPD_OK;
+  if (t.rows > kMost / t.cols) return FOPD_ESHAPE;
   if (t.rows > 1 && (t.ld < t.cols || (with_out && t.ld_out < t.cols))) return FOPD_ESHAPE;
   if (t.grad == nullptr || (with_out && t.out == nullptr)) return FOPD_EINVAL;
   if (with_out && t.out == t.grad && (t.dt != t.dt_out || (t.rows > 1 && t.ld != t.ld_out))) return FOPD_EINVAL;
@@ -1996,6 +1998,7 @@ fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ld
   if (st != FOPD_OK) return st;
   st = check_mx4(weight, weight_bytes, V, d);
   if (st != FOPD_OK) return st;
+  if (V > kMxMaxVocabulary) return FOPD_ESHAPE;
   if (workspace == nullptr || misaligned(workspace, 256) || workspace_bytes < fopd_mx4_logits_workspace_bytes(T, V, d))
     return FOPD_EWORKSPACE;
   if (T == 0) return FOPD_OK;

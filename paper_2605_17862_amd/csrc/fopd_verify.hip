@@ -296,7 +296,7 @@ fopd_verify_rows(VerifyArgs a, int splits, int piece_vecs, RowPart* __restrict__
   const RowPart p = {top, others, sh_at, 0};
   const int64_t at = (drafter ? a.rows : 0) + r;
   parts[at * splits + piece] = p;
-  if (x_id >= begin * E && x_id < a.V && (x_id < (begin + piece_vecs) * E || last_piece)) drafted[at] = load_elem<DT>(row, x_id);
+  if (x_id >= begin * E && x_id < (last_piece ? a.V : end * E)) drafted[at] = load_elem<DT>(row, x_id);
 }
 
 // Workgroup (B - 1 - sample) pieces + piece: the samples whose rows were read last come first.  Every workgroup of a sample makes the sample's decisions, the first one writes them down;

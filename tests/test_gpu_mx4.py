@@ -98,6 +98,19 @@ def test_infinities_and_nan_make_their_block_nan_and_no_other():
     assert bool(nan[[3, 66, 69]].all()) and int(nan.sum()) == 300
 
 
+def test_a_row_that_is_nan_among_few():
+    """The same for the kernel of few rows, and a weight row that is NaN."""
+    h, _ = _matrix(20, 300, "f32", seed=7)
+    h[17, 299] = float("inf")
+    w, _ = _matrix(130, 300, "bf16", seed=8)
+    w[129, 0] = float("nan")
+    z = torch.zeros(20, 136, device=DEV)
+    fb.fopd_mx4_logits(h, fb.FOPD_F32, h.shape[1], _pack(w, "bf16", 130, 300), 20, 130, 300, z, fb.FOPD_F32, 136,
+                       _workspace(fb.fopd_mx4_logits_workspace_bytes(20, 130, 300)))
+    nan = torch.isnan(z[:, :130])
+    assert bool(nan[17].all()) and bool(nan[:, 129].all()) and int(nan.sum()) == 130 + 19
+
+
 def _logits(T, V, d, kind_h, kind, seed, h_pitch=None):
     hb, hx = _matrix(T, d, kind_h, seed, spread=2, pitch=h_pitch)
     wb, wx = _matrix(V, d, "bf16", seed + 1, spread=2)

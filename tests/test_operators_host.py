@@ -59,6 +59,7 @@ def test_mx4_rejects_bad_arguments_before_launch():
     assert logits(ld=96) == 2
     assert logits(ld=101) == 3
     assert logits(w=8192 + 4) == 3
+    assert logits(V=(1 << 28) + 64, ld=(1 << 28) + 64, wn=1 << 62) == 2
     assert logits(wn=fb.fopd_mx4_bytes(100, 64) - 1) == 5
     assert logits(ws=None) == 5
     assert logits(ws=4096 + 16) == 5
@@ -135,6 +136,8 @@ def test_gradient_calls_reject_bad_arguments_before_launch():
         assert call([_entry(rows=2, ld=63)]) == 2
         assert call([_entry(rows=-1)]) == 2
         assert call([_entry(cols=1 << 41, ld=1 << 41)]) == 2
+        assert call([_entry(rows=1 << 39, cols=1 << 39, ld=1 << 39)]) == 2
+        assert call([_entry(rows=1 << 62, cols=4, ld=4)]) == 2
         assert call([_entry(grad=4096 + 2, out=8192)]) == 3
     assert lib.fopd_grad_norm(None, 1, 0, P(4096), None, P(4096), 1 << 20, None) == 1
     assert lib.fopd_grad_clip(None, 1, P(4096), 1.0, 0.0, None, None) == 1
