@@ -728,9 +728,14 @@ struct VerifyPlan {
   size_t parts, drafted, races, total;
   VerifyPlan(int64_t R, int64_t V, int32_t B) {
     const int64_t rows = R < 1 ? 1 : R, samples = B < 1 ? 1 : B;
+    // (as many workgroups as the chip holds at once, none of fewer than 2048 entries; see launch_verify)
     splits = 1;
     while (splits < kVerifyMaxSplits && splits * rows < 2048 && V / (2 * splits) >= 2048) splits *= 2;
-    pieces = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((V + 4095) / 4096, 16), 1024 / samples)));
+    // a race's workgroups end with two atomics each on the sample's state, one after the other, so more of them pay only where the
+    // samples are too few to fill the chip: 8 / 16 / 32 pieces, 1 sample x 151,936 19.2 / 17.3 / 16.3 us, 2 x 262,144 - / 19.0 / 17.0, 8 x
+    // 151,936 22.4 / 19.2 / 19.9, 16 26.2 / 23.8 / 25.7
+    const int64_t most = samples <= 4 ? 32 : 16;
+    pieces = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((V + 4095) / 4096, most), 1024 / samples)));
     size_t off = 256;
     parts = Workspace::take(off, 2 * static_cast<size_t>(rows) * splits * sizeof(RowPart));
     drafted = Workspace::take(off, 2 * static_cast<size_t>(rows) * sizeof(float));
@@ -743,8 +748,12 @@ template <int DT>
 fopd_status launch_verify(const VerifyArgs& a, const VerifyPlan& plan, void* ws, hipStream_t s) {
   const int nvec = a.V / Elem<DT>::kPerVec;
   const unsigned units = static_cast<unsigned>(a.B) * static_cast<unsigned>(a.K + 1) * (a.draft != nullptr ? 2u : 1u);
+  // Three to six workgroups a compute unit; each costs its start and its reductions.  384 / 768 / 1536 of them at least, us: 16 samples of 4
+  // drafts x 151,936 23.8 / 23.8 / 26.0, 8 19.0 / 19.2 / 22.5, 64 of 4 x 32,000 20.4 / 20.9 / 23.2, 64 x 151,936 56.8 / 52.3 / 55.8; 37
+  // looked-up drafts of 0 - 5 x 262,144, whose places are half empty, 34.7 / 32.3 / 30.2.
   int splits = 1;
   while (splits < plan.splits && static_cast<int64_t>(units) * splits < 768) splits *= 2;
+  // the last 200 MB of rows are left in the Infinity Cache for the race: 192 samples 188.8 -> 186.5 us, looked-up drafts 35.3 -> 32.3
   const int64_t cached = (200LL << 20) / (static_cast<int64_t>(a.V) * Elem<DT>::kBytes) * splits, groups = static_cast<int64_t>(units) * splits;
   RowPart* parts = at<RowPart>(ws, plan.parts);
   RaceState* races = at<RaceState>(ws, plan.races);
