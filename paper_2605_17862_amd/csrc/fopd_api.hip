@@ -751,8 +751,11 @@ fopd_status launch_verify(const VerifyArgs& a, const VerifyPlan& plan, void* ws,
   // Three to six workgroups a compute unit; each costs its start and its reductions.  384 / 768 / 1536 of them at least, us: 16 samples of 4
   // drafts x 151,936 23.8 / 23.8 / 26.0, 8 19.0 / 19.2 / 22.5, 64 of 4 x 32,000 20.4 / 20.9 / 23.2, 64 x 151,936 56.8 / 52.3 / 55.8; 37
   // looked-up drafts of 0 - 5 x 262,144, whose places are half empty, 34.7 / 32.3 / 30.2.
+  // Nor more pieces of a sample's rows than a workgroup of the race has lanes, which puts them together: one sample of 8 drafts, at most 64 / 32
+  // / 16 pieces a row, 20.2 / 16.3 / 14.9 us; 4 samples of 4 18.8 / 18.7 / 17.1.
+  const int64_t of_sample = units / static_cast<unsigned>(a.B);
   int splits = 1;
-  while (splits < plan.splits && static_cast<int64_t>(units) * splits < 768) splits *= 2;
+  while (splits < plan.splits && units * static_cast<int64_t>(splits) < 768 && of_sample * 2 * splits <= kVerifyThreads) splits *= 2;
   // the last 200 MB of rows are left in the Infinity Cache for the race: 192 samples 188.8 -> 186.5 us, looked-up drafts 35.3 -> 32.3
   const int64_t cached = (200LL << 20) / (static_cast<int64_t>(a.V) * Elem<DT>::kBytes) * splits, groups = static_cast<int64_t>(units) * splits;
   RowPart* parts = at<RowPart>(ws, plan.parts);
