@@ -4,9 +4,11 @@
 //                           adds the workgroups' sums up, in their order: sum of squares and norm
 //   fopd_grad_scale         out = c grad,  c = min(1, max_norm / (norm + eps))
 //
-// Bound by HBM: the norm reads the list once, the scaling reads it and writes it.  Squares are formed and added in 64 bits, at
-// the rate of 32-bit fused multiply-adds on this part: entries of 1e-30 or 1e30 neither vanish nor overflow, and the result
-// does not depend on the size of the list.
+// Bound by HBM: the norm reads the list once, the scaling reads it and writes it.  622 M fp32 entries: 345 us (7.2 TB/s, the end
+// of the list out of the Infinity Cache on repeated calls) and 882 us (5.6 TB/s, the rate of the fastest copy).  Squares are formed and
+// added in 64 bits, at the rate of 32-bit fused multiply-adds on this part: entries of 1e-30 or 1e30 neither vanish nor overflow, and
+// the result does not depend on the size of the list.  Outputs leave by non-temporal stores (ordinary ones 1359 us for both
+// calls, so 1250), and so do inputs come in the scaling (ordinary loads 1305).
 //
 // A launch gets up to kGradTable tensors by value, in its kernel arguments: nothing is copied to the device beforehand, and a
 // captured launch keeps its own table.  A tensor is rows of `cols` entries; rows that follow each other without a gap are one

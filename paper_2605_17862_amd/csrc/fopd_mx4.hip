@@ -1,7 +1,7 @@
 // Matrices in microscaled 4-bit floating point, and their product on the matrix cores of gfx950 (CDNA4).
 //
 //   fopd_mx4_pack       rows of fp32 / bf16 into blocks of 32 entries that share a power of two
-//   fopd_mx4_unpack     the values of a packed matrix
+//   fopd_mx4_unpack     the values of a packed matrix (both bound by HBM: [151,936, 4096] in bf16 245 - 252 us each, 6.3 TB/s)
 //   fopd_mx4_few        Out[t, v] = sum_k H[t, k] W[v, k] for few rows of H: the weight streamed past them once
 //   fopd_mx4_tiles      the same for many rows, in 256 x 256 tiles
 //
@@ -300,6 +300,15 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
 //     2     B1                 A0 x B1      B0 and scales of the next but one     A1 of this step                    (12 loads stay in flight)
 //     3     A1                 A1 x B1      A0 of the next but one
 //     4                        A1 x B0      B1 of the next but one                B0, scales, A0, B1 of the next step    (9)
+
+// 4096 rows x 151,936, d = 4096: 1.19 - 1.25 ms = 4.1 - 4.3 PFLOP/s (three times the rate of a large bf16 product), d = 32,768 4.85; the instruction
+// alone, operands in registers, reaches 8.7.  Counters: 2.0 GHz, matrix cores 0.51 busy, LDS conflicts 3.5 %; with all loads to one
+// step, so from the L2, 6 % less time: what is left is the slots, in which four wavefronts' reads through the LDS take as long as the
+// other four's products.  Slower or no faster: the 32 x 32 x 64 instruction with a layout for it (9.8 PFLOP/s alone; 1246 us where this took
+// 1219, and 45 rows 78 us where fopd_mx4_few took 70), B0 and the scales read a phase ahead, in the phase without reads (1242 /
+// 1234), four wavefronts of 128 x 128, whose LDS reads are a third fewer but whose requests hold up the only
+// wavefront a SIMD has (1310 / 1225; walking the tiles, with spilled registers, 1454), non-temporal loads of the weight (1287 / 1244; with one tile
+// of rows 3 % faster).  Codes row by row instead of in fragments: 1240 / 1220.
 
 constexpr int kMxScaleLds = 8 * 1024;                     // scales of a step (half of each 1 KB is not read)
 constexpr int kMxTileLds = kLoopLdsBytes + 2 * kMxScaleLds;

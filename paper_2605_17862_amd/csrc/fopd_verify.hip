@@ -10,9 +10,13 @@
 // running sum over the vocabulary, whose borders would have to be known to far more digits than the terms have, and splits over
 // any number of workgroups; the lowest index wins a tie.  tau = 0: the largest logit instead of either.
 //
-// Bound by HBM: every row is read once by the first kernel, and one row of either kind again, mostly from the Infinity Cache,
-// together with the variates by the second.
-
+// Bound by HBM where there are many samples: every row is read once by the first kernel, and one row of either kind again by the
+// second, with the variates.  192 samples of 7 drafts x 151,936 in bf16: rows 145 - 151 us (875 MB, 5.8 - 6.0 TB/s), race 42 us (234 MB,
+// 200 MB of rows left in the Infinity Cache on purpose: 219 MB fetched).  Bound by latency where there are few: one sample of 4 drafts
+// 5 + 8 us, of which reading its 3.3 MB would be 0.5.  A batch of two 16-byte vectors a lane is the best of 2, 4 and 8 (37 samples of up to
+// 5 looked-up drafts x 262,144: 32.2 / 34.4 / 37.8 us), and asking for the next one ahead of this one's arithmetic is slower
+// (34.2).
+//
 #ifndef FOPD_VERIFY_HIP_
 #define FOPD_VERIFY_HIP_
 
