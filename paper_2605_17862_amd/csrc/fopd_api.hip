@@ -682,7 +682,10 @@ fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d,
 // token; a larger one is read past it.  16 rows, d = 4096, call after call, ordinary / non-temporal: 4096 entries (8 rows) 10.8 / 14.7 us,
 // 32,000 16.1 / 19.6, 70,000 (two weights in turn, 305 MB) 34.1 / 31.0, 100,000 47.0 / 41.3; one row x 151,936 61.2 / 54.1.
 constexpr int64_t kMxCachedBytes = 128LL << 20;
-constexpr int64_t kMxFewRows = 64;
+// Blocks of 64 x 64 results up to which fopd_mx4_few is the faster one, whose workgroups spread over the chip where there are few tiles of 256 x
+// 256; with more of them the weight is read too often.  Blocks / it / tiles, us: d = 4096 256 12.3 / 31.9, 512 16.1 / 34.0, 1000 29.0 / 34.1, 1024
+// 25.9 / 38.4, 2000 53.1 / 38.5, 2048 44.9 / 39.6; d = 1024 1000 15.9 / 25.0; d = 512 2504 24.5 / 16.1.
+constexpr int64_t kMxFewGroups = 1536;
 constexpr int64_t kMxMaxVocabulary = 1LL << 28;           // (a launch has at most 2^32 lanes)
 
 // launch(type, whether the weight is read by ordinary loads), both as types.
@@ -697,7 +700,8 @@ fopd_status mx4_variant(fopd_dtype dt, bool cached, Launch launch) {
 // weight [V, d] and hidden rows [T, d], both packed.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
-  if (T > kMxFewRows) {
+  const int64_t few = ((V + 63) / 64) * ((T + 63) / 64);    // workgroups of fopd_mx4_few
+  if (T > 64 && few > kMxFewGroups) {
     const int tiles_m = static_cast<int>((V + kGemmTile - 1) / kGemmTile), tiles_n = static_cast<int>((T + kGemmTile - 1) / kGemmTile);
     const bool walk = gemm_walks(static_cast<int64_t>(tiles_m) * tiles_n, Mx4Layout(V, d).steps, false);
     auto tiles = dt == FOPD_BF16 ? (walk ? fopd_mx4_tiles<FOPD_BF16, true> : fopd_mx4_tiles<FOPD_BF16, false>)
@@ -708,13 +712,13 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
     tiles<<<gemm_grid((tile_groups(tiles_m, tiles_n) + 7) / 8, walk), kLmThreads, kMxTileLds, s>>>(w, V, h, T, d, out, ldo, tiles_m, tiles_n);
     return launched();
   }
-  const int blocks = static_cast<int>(T + 15) / 16;
+  const int blocks = static_cast<int>(std::min<int64_t>((T + 15) / 16, 4));
   return mx4_variant(dt, Mx4Layout(V, d).total <= kMxCachedBytes, [&](auto dt_tag, auto cached_tag) {
     constexpr int DT = decltype(dt_tag)::value;
     constexpr bool CACHED = decltype(cached_tag)::value;
     auto kern = blocks == 1 ? fopd_mx4_few<DT, 1, CACHED> : blocks == 2 ? fopd_mx4_few<DT, 2, CACHED>
                 : blocks == 3 ? fopd_mx4_few<DT, 3, CACHED> : fopd_mx4_few<DT, 4, CACHED>;
-    kern<<<static_cast<unsigned>((V + 63) / 64), kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
+    kern<<<dim3(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((T + 63) / 64)), kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
     return launched();
   });
 }

@@ -204,7 +204,8 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
   }
 }
 
-// Up to 64 rows of H: workgroup x has vocabulary rows 64 x .. + 63.  Its wavefronts take the steps in turn and their sums are added
+// Few rows of H, or few of W: workgroup (x, y) has vocabulary rows 64 x .. + 63 and the up to 64 rows 64 y .. of H, 16 BLOCKS of them
+// at most.  Its wavefronts take the steps in turn and their sums are added
 // in the LDS; the weight goes from memory to the registers of the one wavefront that needs it.  Bound by HBM: one row 48 us = 6.8
 // TB/s; with results to write the rate falls to that of mixed traffic, 45 rows (14 MB of bf16) 65 us = 5.3 TB/s.  Results of 49 - 64
 // rows past the caches: 80 -> 74.5 us, of fewer no faster (30 rows 63.8 / 65.1).  (H in the LDS of one workgroup a compute unit, whose
@@ -218,15 +219,16 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
   __shared__ __align__(16) float sums[kWaves / 2][16 * BLOCKS][64 + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int steps = static_cast<int>(Mx4Layout(V, d).steps);
-  const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64;
+  const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64, t0 = static_cast<int64_t>(blockIdx.y) * 64;
   const unsigned char* w = W + (v0 >> 6) * steps * kMxStepBytes;
+  const unsigned char* h = H + (t0 >> 6) * steps * kMxStepBytes;
   f32x4 acc[4][BLOCKS];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int s = wave; s < steps; s += kWaves) {
-    const unsigned char *ws = w + static_cast<int64_t>(s) * kMxStepBytes, *hs = H + static_cast<int64_t>(s) * kMxStepBytes;
+    const unsigned char *ws = w + static_cast<int64_t>(s) * kMxStepBytes, *hs = h + static_cast<int64_t>(s) * kMxStepBytes;
     i32x4 a[4][2], b[BLOCKS][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -269,8 +271,8 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
     f32x4 z = *reinterpret_cast<const f32x4*>(&sums[0][t][v]);
 #pragma unroll
     for (int u = 1; u < kWaves / 2; ++u) z += *reinterpret_cast<const f32x4*>(&sums[u][t][v]);
-    if (t >= T || v0 + v >= V) continue;
-    char* o = static_cast<char*>(out) + (t * ldo + v0 + v) * Elem<DT>::kBytes;
+    if (t0 + t >= T || v0 + v >= V) continue;
+    char* o = static_cast<char*>(out) + ((t0 + t) * ldo + v0 + v) * Elem<DT>::kBytes;
     if (v0 + v + 4 <= V) {
       typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
       u32x2* o16 = reinterpret_cast<u32x2*>(o);

@@ -78,6 +78,18 @@ def test_every_border_between_two_values(kind):
     assert (out.double().cpu().numpy() == oo.mx4_blocks(buf.double().cpu().numpy())[2]).all()
 
 
+def test_a_row_that_is_nan_among_many():
+    h, _ = _matrix(1300, 300, "bf16", seed=9)
+    h[1100, 299] = float("inf")
+    w, _ = _matrix(6000, 300, "bf16", seed=10)
+    w[5999, 0] = float("nan")
+    z = torch.zeros(1300, 6000, device=DEV)
+    fb.fopd_mx4_logits(h, fb.FOPD_BF16, h.shape[1], _pack(w, "bf16", 6000, 300), 1300, 6000, 300, z, fb.FOPD_F32, 6000,
+                       _workspace(fb.fopd_mx4_logits_workspace_bytes(1300, 6000, 300)))
+    nan = torch.isnan(z)
+    assert bool(nan[1100].all()) and bool(nan[:, 5999].all()) and int(nan.sum()) == 6000 + 1299
+
+
 def test_infinities_and_nan_make_their_block_nan_and_no_other():
     buf, x = _matrix(70, 320, "bf16", seed=5)
     buf[3, 40] = float("inf")
@@ -138,7 +150,8 @@ def _check(z, hx, wx, T, V, d, kind):
 @pytest.mark.parametrize("kind_h,kind", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
 @pytest.mark.parametrize("T,V,d", [(1, 1, 1), (1, 64, 256), (2, 65, 33), (15, 100, 300), (16, 1000, 512), (17, 130, 1024), (33, 255, 700),
                                    (64, 257, 256), (65, 64, 2000), (100, 300, 520), (255, 600, 257), (256, 256, 256), (257, 513, 300), (300, 1030, 1536),
-                                   (1000, 777, 96)])
+                                   (1000, 777, 96), (1500, 4000, 64), (65, 50001, 33), (257, 25000, 300), (2049, 4100, 257),
+                                   (1100, 6003, 513)])
 def test_product_against_the_oracle(T, V, d, kind_h, kind):
     z, hx, wx, _ = _logits(T, V, d, kind_h, kind, seed=T + V)
     _check(z, hx, wx, T, V, d, kind)
@@ -150,7 +163,7 @@ def test_product_of_many_tiles(T, V, d, kind):
     _check(z, hx, wx, T, V, d, kind)
 
 
-@pytest.mark.parametrize("T,V,d", [(3, 1000, 512), (300, 5000, 768)])
+@pytest.mark.parametrize("T,V,d", [(3, 1000, 512), (300, 5000, 768), (1100, 6003, 513)])
 def test_product_twice_captured_and_on_another_stream_gives_the_same_bits(T, V, d):
     z, hx, wx, args = _logits(T, V, d, "bf16", "bf16", seed=9)
     first = z.clone()
@@ -179,7 +192,7 @@ def test_product_twice_captured_and_on_another_stream_gives_the_same_bits(T, V, 
 
 
 def test_two_products_at_once_with_a_workspace_each():
-    one, other = (_logits(T, 3000, 512, "bf16", "f32", seed=s) for T, s in ((5, 1), (270, 2)))
+    one, other = (_logits(T, 3000, 512, "bf16", "f32", seed=s) for T, s in ((5, 1), (2300, 2)))
     torch.cuda.synchronize()
     want = [one[0].clone(), other[0].clone()]
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
