@@ -684,8 +684,8 @@ fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d,
 constexpr int64_t kMxCachedBytes = 128LL << 20;
 // Blocks of 64 x 64 results up to which fopd_mx4_few is the faster one, whose workgroups spread over the chip where there are few tiles of 256 x
 // 256; with more of them the weight is read too often.  Blocks / it / tiles, us: d = 4096 256 12.3 / 31.9, 512 16.1 / 34.0, 1000 29.0 / 34.1, 1024
-// 25.9 / 38.4, 2000 53.1 / 38.5, 2048 44.9 / 39.6; d = 1024 1000 15.9 / 25.0; d = 512 2504 24.5 / 16.1.
-constexpr int64_t kMxFewGroups = 1536;
+// 25.9 / 38.4, 1500 42.1 / 38.2, 1408 34.8 / 38.5, 2000 53.1 / 38.5, 2048 44.9 / 39.6; d = 1024 1000 15.9 / 25.0; d = 512 2504 24.5 / 16.1.
+constexpr int64_t kMxFewGroups = 1280;
 constexpr int64_t kMxMaxVocabulary = 1LL << 28;           // (a launch has at most 2^32 lanes)
 
 // launch(type, whether the weight is read by ordinary loads), both as types.
