@@ -697,6 +697,25 @@ fopd_status mx4_variant(fopd_dtype dt, bool cached, Launch launch) {
   return cached ? launch(F32(), std::true_type()) : launch(F32(), std::false_type());
 }
 
+// Few hidden rows are quantised by the workgroups that use them, each for itself, and the launch that packs them falls away; with many
+// results the workgroups, each of which reads all rows again, take longer than that launch.  Rows x V, d = 4096, quantised by the workgroups /
+// packed first, us: 1 x 4096 7.7 / 10.4, 16 x 8192 10.7 / 11.1, 8 x 16384 12.6 / 11.9, 16 x 16384 13.1 / 12.0, 4 x 32000 14.6 / 15.3, 16 x 32000
+// 17.8 / 15.5, 2 x 64000 24.7 / 25.0, 8 x 64000 28.6 / 25.4, 1 / 2 / 4 / 16 x 151,936 52.7 / 52.9 / 55.1 / 82.0 and 53.8 / 53.9 / 54.4 / 57.4;
+// d = 1024 16 x 16384 7.6 / 10.3.
+bool mx4_raw_rows(int64_t T, int64_t V) { return T <= 2 || (T <= 16 && T * V <= 1 << 17); }
+
+// weight [V, d] packed, the few hidden rows as they are.
+fopd_status launch_mx4_raw(const unsigned char* w, int64_t V, const void* h, fopd_dtype dt_h, int64_t ldh, int64_t T, int64_t d, void* out,
+                           fopd_dtype dt, int64_t ldo, hipStream_t s) {
+  return mx4_variant(dt, Mx4Layout(V, d).total <= kMxCachedBytes, [&](auto dt_tag, auto cached_tag) {
+    constexpr int DT = decltype(dt_tag)::value;
+    constexpr bool CACHED = decltype(cached_tag)::value;
+    auto kern = dt_h == FOPD_BF16 ? fopd_mx4_few<DT, 1, CACHED, FOPD_BF16> : fopd_mx4_few<DT, 1, CACHED, FOPD_F32>;
+    kern<<<static_cast<unsigned>((V + 63) / 64), kMxThreads, 0, s>>>(w, V, h, ldh, T, d, out, ldo);
+    return launched();
+  });
+}
+
 // weight [V, d] and hidden rows [T, d], both packed.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
@@ -718,7 +737,7 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
     constexpr bool CACHED = decltype(cached_tag)::value;
     auto kern = blocks == 1 ? fopd_mx4_few<DT, 1, CACHED> : blocks == 2 ? fopd_mx4_few<DT, 2, CACHED>
                 : blocks == 3 ? fopd_mx4_few<DT, 3, CACHED> : fopd_mx4_few<DT, 4, CACHED>;
-    kern<<<dim3(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((T + 63) / 64)), kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
+    kern<<<dim3(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((T + 63) / 64)), kMxThreads, 0, s>>>(w, V, h, 0, T, d, out, ldo);
     return launched();
   });
 }
@@ -2019,6 +2038,7 @@ fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ld
     return FOPD_EWORKSPACE;
   if (T == 0) return FOPD_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (mx4_raw_rows(T, V)) return launch_mx4_raw(static_cast<const unsigned char*>(weight), V, hidden, dt_hidden, ldh, T, d, logits, dt, ld, s);
   unsigned char* packed = at<unsigned char>(workspace, 256);
   st = launch_mx4_pack(hidden, dt_hidden, T, d, ldh, packed, s);
   if (st != FOPD_OK) return st;

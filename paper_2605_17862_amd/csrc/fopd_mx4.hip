@@ -60,6 +60,35 @@ __host__ __device__ __forceinline__ int mx_code_at(int row, int k) {
 }
 __host__ __device__ __forceinline__ int mx_scale_at(int row, int b) { return kMxCodeBytes + 8 * (16 * (b & 3) + (row & 15)) + 2 * (row >> 4) + (b >> 2); }
 
+// A block whose largest magnitude has these bits: the power it shares, as it is held (magnitudes order as their bits do, infinities and
+// NaN above the rest: 255), and 2^(127 - that), with which a product is exact wherever it is not rounded to zero anyway.
+__device__ __forceinline__ int mx_block_scale(uint32_t top) {
+  const int exponent = static_cast<int>(top >> 23);
+  return exponent == 255 ? 255 : max(exponent - 2, 0);
+}
+__device__ __forceinline__ float mx_block_factor(int scale) {
+  return scale == 255 ? 0.f : __uint_as_float(static_cast<uint32_t>(254 - scale) << 23);
+}
+// Codes of N (4 or 8) entries; of a block of NaN zeros.
+template <int N>
+__device__ __forceinline__ uint32_t mx_codes(const float* x, int scale) {
+  const float f = mx_block_factor(scale);
+  uint32_t codes = 0;
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0] * f, x[1] * f, 1.f, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * f, x[3] * f, 1.f, 1);
+  if constexpr (N == 8) {
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4] * f, x[5] * f, 1.f, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6] * f, x[7] * f, 1.f, 3);
+  }
+  return scale == 255 ? 0u : codes;
+}
+template <int N>
+__device__ __forceinline__ uint32_t mx_largest(const float* x, uint32_t top) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  return top;
+}
+
 // acc += A B over 128 entries; the scales are bytes SA of sa and SB of sb.
 template <int SA, int SB>
 __device__ __forceinline__ f32x4 mx_multiply(const i32x4& a, const i32x4& b, const f32x4& acc, int sa, int sb) {
@@ -129,26 +158,11 @@ fopd_mx4_pack(const void* __restrict__ in, int64_t ld, int64_t R, int64_t d, uns
     const int in_group = row0 + u * kRows;
     float x[E];
     unpack<DT>(q[u], x);
-    uint32_t top = 0;                                      // magnitudes order as their bits do, infinities and NaN above the rest
-#pragma unroll
-    for (int e = 0; e < E; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+    uint32_t top = mx_largest<E>(x, 0);
 #pragma unroll
     for (int off = 1; off < 32 / E; off <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
-    const int exponent = static_cast<int>(top >> 23);
-    const int scale = exponent == 255 ? 255 : max(exponent - 2, 0);
-    // 2^(127 - scale): a power of two, so the product is exact wherever it is not rounded to zero anyway
-    const float inv = exponent == 255 ? 0.f : __uint_as_float(static_cast<uint32_t>(254 - scale) << 23);
-    uint32_t codes = 0;
-    if constexpr (E == 8) {
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0] * inv, x[1] * inv, 1.f, 0);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * inv, x[3] * inv, 1.f, 1);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4] * inv, x[5] * inv, 1.f, 2);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6] * inv, x[7] * inv, 1.f, 3);
-    } else {
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0] * inv, x[1] * inv, 1.f, 0);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2] * inv, x[3] * inv, 1.f, 1);
-    }
-    if (exponent == 255) codes = 0;
+    const int scale = mx_block_scale(top);
+    const uint32_t codes = mx_codes<E>(x, scale);
     unsigned char* to = bytes + mx_code_at(in_group, part * E);
     if constexpr (E == 8) *reinterpret_cast<uint32_t*>(to) = codes;
     else *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(codes);
@@ -211,17 +225,22 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
 // rows past the caches: 80 -> 74.5 us, of fewer no faster (30 rows 63.8 / 65.1).  (H in the LDS of one workgroup a compute unit, whose
 // wavefronts stream sixteen vocabulary rows each: 1 / 45 / 64 rows 58.6 / 72 / 76 us where this takes 54 / 70 / 75; eight
 // wavefronts a workgroup: 95 for one row, with the codes row by row, where four took 69.)
-template <int DT, int BLOCKS, bool CACHED>
+// RAW (BLOCKS 1): the up to 16 rows of H as they are, of that type with pitch ldh.  A fragment's lane holds one row's block, so it
+// quantises that block by itself, while the weight is on its way, and the launch that packs H falls away.  The same bits either way.
+constexpr int kMxPacked = -1;
+
+template <int DT, int BLOCKS, bool CACHED, int RAW = kMxPacked>
 __global__ void __launch_bounds__(kMxThreads)
-fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
+fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const void* __restrict__ H, int64_t ldh, int64_t T, int64_t d,
              void* __restrict__ out, int64_t ldo) {
+  static_assert(RAW == kMxPacked || BLOCKS == 1, "sixteen rows at most");
   constexpr int kWaves = kMxThreads / 64;
   __shared__ __align__(16) float sums[kWaves / 2][16 * BLOCKS][64 + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int steps = static_cast<int>(Mx4Layout(V, d).steps);
   const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64, t0 = static_cast<int64_t>(blockIdx.y) * 64;
   const unsigned char* w = W + (v0 >> 6) * steps * kMxStepBytes;
-  const unsigned char* h = H + (t0 >> 6) * steps * kMxStepBytes;
+  const unsigned char* h = static_cast<const unsigned char*>(H) + (RAW == kMxPacked ? (t0 >> 6) * steps * kMxStepBytes : 0);
   f32x4 acc[4][BLOCKS];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -235,11 +254,50 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const unsigned char
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) a[i][ks] = __builtin_bit_cast(i32x4, load_vec<CACHED>(reinterpret_cast<const u32x4*>(ws + (2 * i + ks) * kMxFragment) + lane));
     const uint2 sa = reinterpret_cast<const uint2*>(ws + kMxCodeBytes)[lane];
+    uint64_t sb;
+    if constexpr (RAW == kMxPacked) {
 #pragma unroll
-    for (int j = 0; j < BLOCKS; ++j)
+      for (int j = 0; j < BLOCKS; ++j)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) b[j][ks] = reinterpret_cast<const i32x4*>(hs + (2 * j + ks) * kMxFragment)[lane];
-    const uint64_t sb = reinterpret_cast<const uint64_t*>(hs + kMxCodeBytes)[lane];
+        for (int ks = 0; ks < 2; ++ks) b[j][ks] = reinterpret_cast<const i32x4*>(hs + (2 * j + ks) * kMxFragment)[lane];
+      sb = reinterpret_cast<const uint64_t*>(hs + kMxCodeBytes)[lane];
+    } else {
+      constexpr int E = Elem<RAW>::kPerVec;
+      const char* row = static_cast<const char*>(H) + std::min<int64_t>(lane & 15, T - 1) * ldh * Elem<RAW>::kBytes;
+      u32x4 raw[2][32 / E];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const int64_t k = static_cast<int64_t>(s) * kMxStep + 128 * ks + 32 * (lane >> 4);
+#pragma unroll
+        for (int c = 0; c < 32 / E; ++c) {
+          const char* p = row + (k + c * E) * Elem<RAW>::kBytes;
+          raw[ks][c] = u32x4{0u, 0u, 0u, 0u};
+          if (k + (c + 1) * E <= d) {
+            raw[ks][c] = *reinterpret_cast<const u32x4*>(p);
+          } else if (k + c * E < d) {
+            float x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = k + c * E + e < d ? load_elem<RAW>(p, e) : 0.f;
+            raw[ks][c] = pack<RAW>(x);
+          }
+        }
+      }
+      sb = 0;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        float x[32];
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < 32 / E; ++c) {
+          unpack<RAW>(raw[ks][c], x + c * E);
+          top = mx_largest<E>(x + c * E, top);
+        }
+        const int scale = mx_block_scale(top);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) b[0][ks][c] = static_cast<int>(mx_codes<8>(x + 8 * c, scale));
+        sb |= static_cast<uint64_t>(scale) << (8 * ks);
+      }
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll

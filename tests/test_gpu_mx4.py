@@ -202,3 +202,24 @@ def test_two_products_at_once_with_a_workspace_each():
                 fb.fopd_mx4_logits(*args)
     torch.cuda.synchronize()
     assert torch.equal(one[0], want[0]) and torch.equal(other[0], want[1])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 777, 20003])
+@pytest.mark.parametrize("d,pitch", [(1, None), (77, 96), (1000, None), (1531, 1536)])
+def test_few_rows_give_the_bits_they_have_among_more(V, d, pitch, kind):
+    """Each sum is taken in one order, however many rows stand beside it and whether the rows are packed first."""
+    h, _ = _matrix(20, d, kind, seed=V + d, pitch=pitch)
+    h[2, d // 2] = float("inf")                                      # NaN results, in a row that few of the calls have
+    h[3, :d] = 0.0
+    h[5, d - 1] = float("nan")
+    w, _ = _matrix(V, d, "bf16", seed=9, spread=2)
+    packed, ld = _pack(w, "bf16", V, d), (V + 3) // 4 * 4
+    rows = {}
+    for T in (20, 16, 8, 6, 2, 1):
+        rows[T] = torch.full((T, ld), 7.0, device=DEV)
+        fb.fopd_mx4_logits(h, KINDS[kind][1], h.shape[1], packed, T, V, d, rows[T], fb.FOPD_F32, ld,
+                           _workspace(fb.fopd_mx4_logits_workspace_bytes(T, V, d)))
+    assert bool(torch.isnan(rows[20][[2, 5], :V]).all()) and not bool(torch.isnan(rows[20][[0, 1, 3, 4, 19]]).any())
+    for T in (16, 8, 6, 2, 1):
+        assert np.array_equal(rows[T].cpu().numpy(), rows[20][:T].cpu().numpy(), equal_nan=True)
