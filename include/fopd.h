@@ -614,7 +614,7 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
  * fopd_mx4_quantize    in [R, ld] of `dt` -> packed; columns d .. ld - 1 are not read
  * fopd_mx4_dequantize  packed -> out [R, ldo] of `dt`; every value that a block of bf16 entries gives is exact in bf16
  * fopd_mx4_logits      logits[t, v] = sum_k hidden[t, k] weight[v, k], both in 4-bit blocks: hidden [T, ldh] of `dt_hidden`
- *                      is quantised on the way (into the workspace), `weight` is the packed [V, d] projection, laid out
+ *                      is quantised on the way (workspace), `weight` is the packed [V, d] projection, laid out
  *                      once.  fp32 sums, rounded once to `dt`; columns V .. ld - 1 of the logits are not written.  What a
  *                      drafter runs for each token it proposes (fopd_verify_draft takes its logits), or a scoring pass
  *                      whose teacher or policy is served with such a projection.
@@ -622,7 +622,7 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
  *   workspace          fopd_mx4_logits_workspace_bytes(T, V, d) bytes, 256-byte aligned; nothing in it has to be initialised
  * The sum over k of a result is taken in an order that goes by T, V and d, not by its place: the same hidden row in a call of
  * another T may differ in its last bits.  The first call in a process sets a kernel attribute: make one call before
- * capturing fopd_mx4_logits into a HIP graph.  T = 0 or R = 0 does nothing.
+ * capturing fopd_mx4_logits into a HIP graph.  T = 0 or R = 0 does nothing.  Outputs share no memory with inputs.
  */
 size_t fopd_mx4_bytes(int64_t R, int64_t d);
 fopd_status fopd_mx4_quantize(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed,
