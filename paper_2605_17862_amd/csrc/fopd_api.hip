@@ -716,10 +716,32 @@ fopd_status launch_mx4_raw(const unsigned char* w, int64_t V, const void* h, fop
   });
 }
 
+// Rows for fopd_mx4_stream, and workgroups of it for most compute units.  The kernel taken without this rule / it, us, d = 4096: 45 x 151,936
+// 65.1 / 65.7; 64 x 32,000 / 40,000 / 151,936 17.8 / 21.0, 24.9 / 21.6, 75.6 / 69.0; 96 x 24,000 / 40,000 / 151,936 26.3 / 24.6, 37.1 / 25.7, 105 /
+// 78.8; 128 x 16,384 / 24,000 / 151,936 15.8 / 27.8, 26.5 / 25.9, 111 / 81.5; 160 x 24,000 / 65,536 / 151,936 37.0 / 29.2, 39.2 / 41.0, 111 / 91.1
+// (of 192 registers spill: 111 / 255); d = 512 128 x 50,000 15.5 / 12.5, d = 16,384 119 / 106.
+bool mx4_streams(int64_t T, int64_t V) { return T > 48 && T <= 160 && V > (T > 64 ? 192 : 256) * MxStream<4>::kVocabulary; }
+
 // weight [V, d] and hidden rows [T, d], both packed.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
   const int64_t few = ((V + 63) / 64) * ((T + 63) / 64);    // workgroups of fopd_mx4_few
+  if (mx4_streams(T, V)) {
+    return mx4_variant(dt, Mx4Layout(V, d).total <= kMxCachedBytes, [&](auto dt_tag, auto cached_tag) {
+      constexpr int DT = decltype(dt_tag)::value;
+      constexpr bool CACHED = decltype(cached_tag)::value;
+      auto go = [&](auto blocks_tag) {
+        using S = MxStream<decltype(blocks_tag)::value>;
+        fopd_mx4_stream<DT, S::kBlocks, CACHED>
+            <<<static_cast<unsigned>((V + S::kVocabulary - 1) / S::kVocabulary), kMxThreads, 0, s>>>(w, V, h, T, d, out, ldo);
+        return launched();
+      };
+      if (T <= 64) return go(std::integral_constant<int, 4>());
+      if (T <= 96) return go(std::integral_constant<int, 6>());
+      if (T <= 128) return go(std::integral_constant<int, 8>());
+      return go(std::integral_constant<int, 10>());
+    });
+  }
   if (T > 64 && few > kMxFewGroups) {
     const int tiles_m = static_cast<int>((V + kGemmTile - 1) / kGemmTile), tiles_n = static_cast<int>((T + kGemmTile - 1) / kGemmTile);
     const bool walk = gemm_walks(static_cast<int64_t>(tiles_m) * tiles_n, Mx4Layout(V, d).steps, false);

@@ -222,7 +222,7 @@ fopd_mx4_unpack(const unsigned char* __restrict__ packed, int64_t R, int64_t d, 
 // at most.  Its wavefronts take the steps in turn and their sums are added
 // in the LDS; the weight goes from memory to the registers of the one wavefront that needs it.  Bound by HBM: one row 48 us = 6.8
 // TB/s; with results to write the rate falls to that of mixed traffic, 45 rows (14 MB of bf16) 65 us = 5.3 TB/s.  Results of 49 - 64
-// rows past the caches: 80 -> 74.5 us, of fewer no faster (30 rows 63.8 / 65.1).  (H in the LDS of one workgroup a compute unit, whose
+// rows past the caches: 64 x 32,000 18.2 -> 17.8 us, 128 x 24,000 in fp32, d = 512, 13.0 -> 11.6, of fewer no faster (30 x 151,936 63.8 / 65.1).  (H in the LDS of one workgroup a compute unit, whose
 // wavefronts stream sixteen vocabulary rows each: 1 / 45 / 64 rows 58.6 / 72 / 76 us where this takes 54 / 70 / 75; eight
 // wavefronts a workgroup: 95 for one row, with the codes row by row, where four took 69.)
 // RAW (BLOCKS 1): the up to 16 rows of H as they are, of that type with pitch ldh.  A fragment's lane holds one row's block, so it
@@ -344,6 +344,150 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const void* __restr
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (v0 + v + e < V) store_elem<DT>(o, e, z[e]);
+    }
+  }
+}
+
+// ---- some rows of H ------------------------------------------------------------------------------------------------
+// Up to 16 BLOCKS rows of H and a workgroup for every 128 vocabulary rows: the weight is read once, by the wavefront that
+// multiplies it (32 rows of it), straight into registers a step of 256 entries ahead; H's step, 8.5 KB of 64 rows, goes through one of two
+// places in the LDS, so the workgroup reads it once where fopd_mx4_few's wavefronts all would.  Two workgroups a compute unit (of 8 blocks:
+// 206 registers; with at most 168, for three, they spill: 297 us where this takes 83).  Bound by HBM, reads and writes mixed: 128 rows x
+// 151,936, d = 4096, 311 MB read and 39 written, 81 us = 4.3 TB/s (fopd_mx4_tiles, half of whose tile is columns that do not exist, 111;
+// fopd_mx4_few with eight blocks 106).  H's loads are asked for first, since they are waited for first, to be placed: the other way round the
+// wait took in the weight's, 128 x 40,000 32.7 us instead of 27.5.  Weights two steps ahead: no faster (128 x 151,936 88).  Ordinary
+// stores: 93.
+template <int BLOCKS>
+struct MxStream {
+  static constexpr int kBlocks = BLOCKS;
+  static constexpr int kGroups = (BLOCKS + 3) / 4;                     // of 64 rows of H
+  static constexpr int kVocabulary = 128;                              // rows of W a workgroup
+  static constexpr int kStage = kGroups * kMxStepBytes;
+  static constexpr int kSums = 64 * (kVocabulary + 4) * 4;
+  static constexpr int kLds = 2 * kStage > kSums ? 2 * kStage : kSums;
+};
+
+template <int DT, int BLOCKS, bool CACHED>
+__global__ void __launch_bounds__(kMxThreads, 2)
+fopd_mx4_stream(const unsigned char* __restrict__ W, int64_t V, const unsigned char* __restrict__ H, int64_t T, int64_t d,
+                void* __restrict__ out, int64_t ldo) {
+  using S = MxStream<BLOCKS>;
+  static_assert(kMxThreads == 4 * 64, "four wavefronts of 32 vocabulary rows");
+  __shared__ __align__(16) unsigned char lds[S::kLds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int steps = static_cast<int>(Mx4Layout(V, d).steps);
+  const int64_t v0 = static_cast<int64_t>(blockIdx.x) * S::kVocabulary;
+  // (groups that do not exist: the last one again, whose results are not written)
+  const unsigned char* w = W + std::min<int64_t>((v0 >> 6) + (wave >> 1), ((V + 63) >> 6) - 1) * steps * kMxStepBytes;
+  const int last_group = static_cast<int>((T + 63) >> 6) - 1;
+  f32x4 acc[2][BLOCKS];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  struct Weight { i32x4 codes[2][2]; uint32_t scales; };
+  constexpr int kVecs = kMxStepBytes / 16;                             // of a step of 64 rows
+  constexpr int kLoads = (S::kGroups * kVecs + kMxThreads - 1) / kMxThreads;
+  auto load_weight = [&](int s, Weight& a) {
+    const unsigned char* ws = w + static_cast<int64_t>(s) * kMxStepBytes;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+        a.codes[i][ks] = __builtin_bit_cast(i32x4, load_vec<CACHED>(reinterpret_cast<const u32x4*>(ws + (4 * (wave & 1) + 2 * i + ks) * kMxFragment) + lane));
+    a.scales = *reinterpret_cast<const uint32_t*>(ws + kMxCodeBytes + 8 * lane + 4 * (wave & 1));
+  };
+  auto load_rows = [&](int s, u32x4 (&h)[kLoads]) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int k = tid + u * kMxThreads, g = k / kVecs;
+      if (k < S::kGroups * kVecs)
+        h[u] = *reinterpret_cast<const u32x4*>(H + (static_cast<int64_t>(min(g, last_group)) * steps + s) * kMxStepBytes + (k - g * kVecs) * 16);
+    }
+  };
+  auto place_rows = [&](int s, const u32x4 (&h)[kLoads]) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int k = tid + u * kMxThreads;
+      if (k < S::kGroups * kVecs) *reinterpret_cast<u32x4*>(lds + (s & 1) * S::kStage + k * 16) = h[u];
+    }
+  };
+  auto meet = [&] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  };
+  auto multiply = [&](int s, const Weight& a) {
+    const unsigned char* hs = lds + (s & 1) * S::kStage;
+#pragma unroll
+    for (int g = 0; g < S::kGroups; ++g) {
+      const uint64_t sb = reinterpret_cast<const uint64_t*>(hs + g * kMxStepBytes + kMxCodeBytes)[lane];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (4 * g + j >= BLOCKS) break;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          const i32x4 b = reinterpret_cast<const i32x4*>(hs + g * kMxStepBytes + (2 * j + ks) * kMxFragment)[lane];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            acc[i][4 * g + j] = mx_multiply(a.codes[i][ks], b, acc[i][4 * g + j], static_cast<int>(a.scales), 2 * i + ks,
+                                            static_cast<int>(j < 2 ? sb : sb >> 32), 2 * (j & 1) + ks);
+        }
+      }
+    }
+  };
+
+  Weight a0, a1;
+  u32x4 h[kLoads];
+  auto step = [&](int s, const Weight& now, Weight& next) {
+    if (s + 1 < steps) {
+      load_rows(s + 1, h);                                               // (they are waited for first)
+      load_weight(s + 1, next);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(s, now);
+    __builtin_amdgcn_sched_barrier(0);
+    if (s + 1 < steps) place_rows(s + 1, h);
+    meet();
+  };
+  load_rows(0, h);
+  load_weight(0, a0);
+  place_rows(0, h);
+  meet();
+  for (int s = 0; s < steps; s += 2) {
+    step(s, a0, a1);
+    if (s + 1 < steps) step(s + 1, a1, a0);
+  }
+  // register r of acc[i][j]: vocabulary row 32 wave + 16 i + 4 (lane / 16) + r, row 16 j + lane % 16 of H; 64 rows at a time
+  float(*sums)[S::kVocabulary + 4] = reinterpret_cast<float(*)[S::kVocabulary + 4]>(lds);
+#pragma unroll
+  for (int g = 0; g < S::kGroups; ++g) {
+    constexpr int kRows = 64;
+    if (g > 0) meet();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (4 * g + j >= BLOCKS) break;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(&sums[16 * j + (lane & 15)][32 * wave + 16 * i + 4 * (lane >> 4)]) = acc[i][4 * g + j];
+    }
+    meet();
+    const int rows = min(kRows, 16 * (BLOCKS - 4 * g));
+    for (int k = tid; k < rows * (S::kVocabulary / 4); k += kMxThreads) {
+      const int t = k / (S::kVocabulary / 4), v = 4 * (k % (S::kVocabulary / 4));
+      const f32x4 z = *reinterpret_cast<const f32x4*>(&sums[t][v]);
+      if (64 * g + t >= T || v0 + v >= V) continue;
+      char* o = static_cast<char*>(out) + ((64 * g + t) * ldo + v0 + v) * Elem<DT>::kBytes;
+      if (v0 + v + 4 <= V) {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 z16 = {pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+        if constexpr (DT == FOPD_BF16) __builtin_nontemporal_store(z16, reinterpret_cast<u32x2*>(o));
+        else __builtin_nontemporal_store(z, reinterpret_cast<f32x4*>(o));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v0 + v + e < V) store_elem<DT>(o, e, z[e]);
+      }
     }
   }
 }

@@ -223,3 +223,44 @@ def test_few_rows_give_the_bits_they_have_among_more(V, d, pitch, kind):
     assert bool(torch.isnan(rows[20][[2, 5], :V]).all()) and not bool(torch.isnan(rows[20][[0, 1, 3, 4, 19]]).any())
     for T in (16, 8, 6, 2, 1):
         assert np.array_equal(rows[T].cpu().numpy(), rows[20][:T].cpu().numpy(), equal_nan=True)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,d", [(49, 32769, 1), (64, 33000, 256), (65, 40001, 257), (96, 32831, 800), (97, 33003, 513), (128, 32960, 1500), (127, 50001, 33),
+                                   (129, 24577, 600), (160, 24700, 257), (150, 30001, 65)])
+def test_product_of_some_rows_with_a_large_vocabulary(T, V, d, kind):
+    z, hx, wx, _ = _logits(T, V, d, "bf16", kind, seed=T + V + d)
+    _check(z, hx, wx, T, V, d, kind)
+
+
+def test_product_of_some_rows_with_a_weight_that_no_cache_holds():
+    T, V, d = 100, 151936, 1800
+    h, hx = _matrix(T, d, "bf16", seed=3, spread=2)
+    w = torch.randn(V, d, generator=torch.Generator(DEV).manual_seed(4), device=DEV).bfloat16()
+    z = torch.full((T + 1, V + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    fb.fopd_mx4_logits(h, fb.FOPD_BF16, d, _pack(w, "bf16", V, d), T, V, d, z, fb.FOPD_BF16, V + 8,
+                       _workspace(fb.fopd_mx4_logits_workspace_bytes(T, V, d)))
+    at = np.unique(np.r_[0:130, V - 130:V, np.random.default_rng(0).integers(0, V, 500)])
+    _check(torch.cat((z[:, at], z[:, V:]), 1), hx, w[at].double().cpu().numpy(), T, len(at), d, "bf16")
+
+
+def test_some_rows_that_are_nan_captured_and_replayed():
+    T, V, d = 70, 40000, 600
+    z, _, _, args = _logits(T, V, d, "f32", "f32", seed=11)
+    hb = args[0]
+    hb[66, 599] = float("nan")
+    want = torch.empty_like(z)
+    fb.fopd_mx4_logits(*args)
+    want.copy_(z)
+    assert bool(torch.isnan(want[66, :V]).all()) and int(torch.isnan(want).sum()) == V
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        fb.fopd_mx4_logits(*args)
+    for _ in range(3):
+        z[:T, :V] = 0.0
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(z.cpu().numpy(), want.cpu().numpy(), equal_nan=True)
