@@ -353,7 +353,7 @@ fopd_mx4_few(const unsigned char* __restrict__ W, int64_t V, const void* __restr
 // multiplies it (32 rows of it), straight into registers a step of 256 entries ahead; H's step, 8.5 KB of 64 rows, goes through one of two
 // places in the LDS, so the workgroup reads it once where fopd_mx4_few's wavefronts all would.  Two workgroups a compute unit (of 8 blocks:
 // 206 registers; with at most 168, for three, they spill: 297 us where this takes 83).  Bound by HBM, reads and writes mixed: 128 rows x
-// 151,936, d = 4096, 311 MB read and 39 written, 81 us = 4.3 TB/s (fopd_mx4_tiles, half of whose tile is columns that do not exist, 111;
+// 151,936, d = 4096, 331 MB read and 39 written, 76 us = 4.9 TB/s (81 with the launch that packs H; so counted, fopd_mx4_tiles, half of whose tile is columns that do not exist, 111;
 // fopd_mx4_few with eight blocks 106).  H's loads are asked for first, since they are waited for first, to be placed: the other way round the
 // wait took in the weight's, 128 x 40,000 32.7 us instead of 27.5.  Weights two steps ahead: no faster (128 x 151,936 88).  Ordinary
 // stores: 93.
