@@ -102,7 +102,12 @@ struct VerifyLane {
   int batch = -1;
 };
 
-__device__ __forceinline__ float verify_reference(float top, float c) { return fmaxf(top, -1e30f) * c; }
+// As rounded wherever it goes: a difference of references that took in the product unrounded would be a rounding of |top| c away
+// from what the terms were formed with (logits near 1000: 5e-5 of the sum).
+__device__ __forceinline__ float verify_reference(float top, float c) {
+#pragma clang fp contract(off)
+  return fmaxf(top, -1e30f) * c;
+}
 
 template <int N>
 __device__ __forceinline__ float verify_batch(const float* x, float c, float ref) {

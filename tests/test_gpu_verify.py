@@ -372,3 +372,49 @@ def test_from_a_draft_to_clipped_gradients():
     assert abs(float(norm) - want_n) <= 2.0 ** -23 * want_n and abs(float(coef) - want_c) <= 2.0 ** -23 * want_c
     for t, w in zip(grads, want):
         assert (np.abs(t.double().cpu().numpy() - w) <= 2.0 ** -22 * np.abs(w) + 2.0 ** -149).all()
+
+
+def _likely(rows, V, kind, tau, shift, masked=None, low=-1e9):
+    """Rows of one token of probability 1 - 1e-9 or so, the others spread over some 10 tau below; the first `masked` entries `low`."""
+    dtype, dt, per = KINDS[kind]
+    g = torch.Generator().manual_seed(rows + V)
+    z = torch.rand(rows, V, generator=g) * -10.0 - 21.0 - math.log(V)
+    at = torch.randint(masked or 0, V, (rows,), generator=g)
+    z[torch.arange(rows), at] = 0.0
+    z = z * tau + shift
+    if masked:
+        z[:, :masked] = low
+    ld = (V + per - 1) // per * per
+    target = torch.full((rows, ld), float("nan"), dtype=dtype, device=DEV)
+    target[:, :V] = z.to(dtype).to(DEV)
+    return target, at, ld
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(3, 70), (5, 20011), (600, 5003)])
+@pytest.mark.parametrize("tau,shift,masked,low", [
+    (1.0, 0.0, 0, 0.0), (0.05, 3.0, 0, 0.0), (1.0, 100.0, 0, 0.0), (1.0, 1000.0, 0, 0.0), (0.6, 1000.0, 0, 0.0), (1.0, 5.0, 0.6, float("-inf"))])
+def test_log_probs_keep_their_digits_wherever_the_logits_lie(tau, shift, masked, low, rows, V, kind):
+    target, at, ld = _likely(rows, V, kind, tau, shift, int(masked * V), low)
+    taus = torch.full((rows,), tau, device=DEV)
+    noise = torch.ones(rows, (V + 3) // 4 * 4, device=DEV)
+    n, ids = (torch.full((rows,), -9, dtype=torch.int32, device=DEV) for _ in range(2))
+    logp, mask = torch.full((rows,), 9.0, device=DEV), torch.full((rows,), 9, dtype=torch.uint8, device=DEV)
+    ws = _workspace(fb.fopd_verify_workspace_bytes(rows, V, rows))
+    fb.fopd_verify_draft(target, None, KINDS[kind][1], rows, V, ld, ld, None, None, None, rows, 0, taus, None, noise, noise.shape[1],
+                         n, ids, logp, mask, ws)
+    assert fb.fopd_workspace_status(ws) == (0, 0)
+    z = target[:, :V].double().cpu().numpy() / float(taus[0])
+    s = z - z.max(axis=1, keepdims=True)
+    assert (ids.cpu().numpy() == at.numpy()).all() and (mask == 1).all()
+    s[np.arange(rows), at.numpy()] = -math.inf
+    others = np.exp(s).sum(axis=1)                                         # (the bf16 ones near 1000 are 4 apart: ties among them)
+    assert others.max() < 1e-2
+    # a term's exponent t has five roundings relative to itself (log2 e, its division by tau, the multiply-add, and the difference and the
+    # product where pieces meet); up to four exponentials of one unit in the last place (2^-23) multiply up, with as many
+    # products; V / 256 + 64 additions; log1p and the result
+    far = np.where(np.exp(s) > 0, np.abs(s), 0.0).max()
+    tol = 2.0 ** -24 * (5.0 * far + 8.0 + 4.0 + V / 256 + 64 + 2.0)
+    want = -np.log1p(others)
+    off = np.abs(logp.double().cpu().numpy() - want)
+    assert (off <= tol * np.abs(want)).all(), (off / np.maximum(np.abs(want), 1e-300)).max()
