@@ -127,7 +127,8 @@ __device__ __forceinline__ void verify_add(const float* x, float c, int batch, V
   for (int e = 0; e < N; ++e) m = fmaxf(m, x[e]);
   if (m > s.top) {
     const float ref = verify_reference(m, c);
-    s.sum *= static_cast<double>(fast_exp2(s.ref - ref));
+    // (ref only grows, except from an empty sum's 0 to logits below it: no factor there, which may be infinite)
+    s.sum *= static_cast<double>(fast_exp2(fminf(s.ref - ref, 0.f)));
     s.top = m;
     s.ref = ref;
     s.batch = batch;
@@ -289,8 +290,8 @@ fopd_verify_rows(VerifyArgs a, int splits, int piece_vecs, RowPart* __restrict__
   const float to_top = top == kMinusInf ? 1.f : fast_exp2(-fmaf(top, s.c, -ref));
   float others = total(mine.batch < 0 ? static_cast<float>(mine.sum) : static_cast<float>(mine.sum) * fast_exp2(mine.ref - ref) * to_top);
   if (top > kMinusInf && (!(fabsf(top) < 1e30f) || !(fabsf(top * s.c) < 1e38f) || !(others < __builtin_inff()))) {
-    // entries whose product with c is no finite number (rows of the type's lowest value), or NaN among them: again, with the
-    // largest entry subtracted first
+    // a largest entry whose product with c is no finite number (rows of the type's lowest value), or NaN: again, with the
+    // largest entry subtracted first.  (Entries of that size are equal or too far apart to count: the sum is a whole number.)
     float sum = 0.f;
     for (int w = begin + tid; w < end; w += kVerifyThreads) {
       float x[E];

@@ -393,7 +393,9 @@ def _likely(rows, V, kind, tau, shift, masked=None, low=-1e9):
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V", [(3, 70), (5, 20011), (600, 5003)])
 @pytest.mark.parametrize("tau,shift,masked,low", [
-    (1.0, 0.0, 0, 0.0), (0.05, 3.0, 0, 0.0), (1.0, 100.0, 0, 0.0), (1.0, 1000.0, 0, 0.0), (0.6, 1000.0, 0, 0.0), (1.0, 5.0, 0.6, float("-inf"))])
+    (1.0, 0.0, 0, 0.0), (0.05, 3.0, 0, 0.0), (1.0, 100.0, 0, 0.0), (1.0, 1000.0, 0, 0.0), (0.6, 1000.0, 0, 0.0), (1.0, 5.0, 0.6, float("-inf")),
+    (1.0, -150.0, 0, 0.0), (1.0, -1000.0, 0, 0.0), (0.1, -12.0, 0, 0.0),
+    (1.0, 2.0, 0.6, -3.3895313892515355e38), (0.7, -120.0, 0.6, -1e9), (1.0, 0.0, 0.3, -10000.0)])
 def test_log_probs_keep_their_digits_wherever_the_logits_lie(tau, shift, masked, low, rows, V, kind):
     target, at, ld = _likely(rows, V, kind, tau, shift, int(masked * V), low)
     taus = torch.full((rows,), tau, device=DEV)
@@ -418,3 +420,14 @@ def test_log_probs_keep_their_digits_wherever_the_logits_lie(tau, shift, masked,
     want = -np.log1p(others)
     off = np.abs(logp.double().cpu().numpy() - want)
     assert (off <= tol * np.abs(want)).all(), (off / np.maximum(np.abs(want), 1e-300)).max()
+
+
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("shift,taus", [(-150.0, (0.7, 1.0, 0.0)), (-9.0, (0.1, 0.2)), (-1000.0, (1.6,))])
+def test_logits_far_below_zero(shift, taus, draft):
+    b = Batch(21, 4, 5003, "f32", seed=41, draft=draft, taus=taus)
+    b.target += shift
+    if draft:
+        b.draft += shift
+    b.run()
+    b.check(at_least=0.7)
