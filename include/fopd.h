@@ -664,7 +664,8 @@ fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ld
  *   out_ids, out_logp, out_mask   [R] int32, f32, uint8 out: rows 0 .. a of a sample get the token, log p_j(token) and 1, its
  *                  rows behind -1, 0 and 0 (up to max_draft in a padded batch): token_ids, behav_logp and mask of the loss.
  *                  Rows of no sample stay as they were.  Samples must not share rows, nor outputs memory with inputs.
- *   workspace      fopd_verify_workspace_bytes(R, V, B) bytes, 256-byte aligned, initialised once with fopd_workspace_init
+ *   workspace      fopd_verify_workspace_bytes(R, V, B) bytes, 256-byte aligned, initialised once with fopd_workspace_init; it serves
+ *                  any call with at most R rows, V entries and B samples
  *
  * On the device: draft_lens outside 0 .. max_draft or rows outside [0, R) raise FOPD_ESEGMENTS, n_accepted is 0 and no row is
  * written (in a padded batch: -1, 0, 0).  A drafted id outside [0, V) raises FOPD_ETOKEN_RANGE and is not kept.  A row that is

@@ -767,22 +767,29 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
 // ---- verification of drafted tokens ---------------------------------------------------------
 
 // How a call is cut: pieces of a row in the first kernel (a power of two), pieces of a race.  The workspace is asked for with R, V
-// and B, so `splits` is the most that a call of any number of drafts may take.
+// and B, so `splits` is the most that a call of any number of drafts may take.  Fewer rows are cut into more pieces, and a
+// workspace serves every call that is smaller in R, V or B: its size has room for the most pieces that any number of rows
+// up to R comes to.
 struct VerifyPlan {
   int splits, pieces;
   size_t parts, drafted, races, total;
   VerifyPlan(int64_t R, int64_t V, int32_t B) {
     const int64_t rows = R < 1 ? 1 : R, samples = B < 1 ? 1 : B;
     // (as many workgroups as the chip holds at once, none of fewer than 2048 entries; see launch_verify)
+    constexpr int64_t kRowParts = 2048;
+    int64_t most_splits = 1;                               // of a single row
+    while (most_splits < kVerifyMaxSplits && V / (2 * most_splits) >= 2048) most_splits *= 2;
     splits = 1;
-    while (splits < kVerifyMaxSplits && splits * rows < 2048 && V / (2 * splits) >= 2048) splits *= 2;
+    while (splits < most_splits && splits * rows < kRowParts) splits *= 2;
+    // (the last doubling started below kRowParts)
+    const int64_t room = std::min(rows * most_splits, std::max(rows, 2 * kRowParts));
     // a race's workgroups end with two atomics each on the sample's state, one after the other, so more of them pay only where the
     // samples are too few to fill the chip: 8 / 16 / 32 pieces, 1 sample x 151,936 19.2 / 17.3 / 16.3 us, 2 x 262,144 - / 19.0 / 17.0, 8 x
     // 151,936 22.4 / 19.2 / 19.9, 16 26.2 / 23.8 / 25.7
     const int64_t most = samples <= 4 ? 32 : 16;
     pieces = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((V + 4095) / 4096, most), 1024 / samples)));
     size_t off = 256;
-    parts = Workspace::take(off, 2 * static_cast<size_t>(rows) * splits * sizeof(RowPart));
+    parts = Workspace::take(off, 2 * static_cast<size_t>(room) * sizeof(RowPart));
     drafted = Workspace::take(off, 2 * static_cast<size_t>(rows) * sizeof(float));
     races = Workspace::take(off, static_cast<size_t>(samples) * sizeof(RaceState));
     total = off;

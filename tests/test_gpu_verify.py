@@ -431,3 +431,18 @@ def test_logits_far_below_zero(shift, taus, draft):
         b.draft += shift
     b.run()
     b.check(at_least=0.7)
+
+
+def test_smaller_batches_in_the_workspace_of_a_larger_one():
+    """The batch shrinks as its samples end, and the workspace stays."""
+    V = 9000
+    n = fb.fopd_verify_workspace_bytes(2048, V, 256)
+    guarded = _workspace(n + 4096)
+    ws = guarded[:n]
+    guarded[n:] = 77
+    for B, K in ((255, 7), (128, 7), (127, 7), (16, 3), (1, 0)):
+        b = Batch(B, K, V, "bf16", seed=42, taus=(0.7,))
+        b.run(ws)
+        b.ws = ws
+        b.check(at_least=0.7 if B > 1 else 0.0)
+    assert bool((guarded[n:] == 77).all())

@@ -104,6 +104,20 @@ def test_verification_rejects_bad_arguments_before_launch():
     assert need % 256 == 0 and _verify(lib, wsn=need - 1) == 5
 
 
+@pytest.mark.parametrize("V", [1, 4095, 4096, 8191, 8192, 32000, 151936, 262144])
+def test_a_workspace_for_a_verification_serves_every_smaller_one(V):
+    """Around the row counts where a row is cut into half as many pieces, and over all sizes in between."""
+    sizes = sorted({max(1, n + k) for n in [1 << e for e in range(17)] + [248, 1016, 1536] for k in (-1, 0, 1)})
+    need = [fb.fopd_verify_workspace_bytes(R, V, 5) for R in sizes]
+    assert need == sorted(need)
+    need = [fb.fopd_verify_workspace_bytes(1000, V, B) for B in sizes]
+    assert need == sorted(need)
+    need = [fb.fopd_verify_workspace_bytes(R, v, 5) for R in (1, 2, 31, 33, 1023) for v in (V // 2 + 1, V, V + 1, 2 * V)]
+    assert all(need[k:k + 4] == sorted(need[k:k + 4]) for k in range(0, len(need), 4))
+    # a ragged batch of fewer samples, as the rollouts end
+    assert max(fb.fopd_verify_workspace_bytes(8 * B, V, B) for B in range(1, 257)) == fb.fopd_verify_workspace_bytes(2048, V, 256)
+
+
 def test_status_of_a_row_without_a_distribution():
     assert fb.fopd_flags_status(16) == 12
     assert fb.fopd_flags_status(17) == 6
