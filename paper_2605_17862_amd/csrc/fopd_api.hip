@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -256,17 +257,19 @@ inline Options current_options() {
 constexpr size_t kLdsPerCu = 160 * 1024;
 
 // A kernel that wants more dynamic LDS than the default limit has to be told so once per device.
-// `done` is the caller's per-kernel table of devices already told.
+// `done` is the caller's table, for these kernels, of devices already told.
 constexpr int kMaxDevices = 64;
-inline fopd_status allow_dynamic_lds(const void* kern, int bytes, bool* done) {
+inline fopd_status allow_dynamic_lds(std::initializer_list<const void*> kernels, int bytes, bool* done) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return FOPD_EHIP;
   std::lock_guard<std::mutex> lock(g_state_mutex);
   if (done[dev]) return FOPD_OK;
-  if (hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return FOPD_EHIP;
+  for (const void* kern : kernels)
+    if (hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return FOPD_EHIP;
   done[dev] = true;
   return FOPD_OK;
 }
+inline fopd_status allow_dynamic_lds(const void* kern, int bytes, bool* done) { return allow_dynamic_lds({kern}, bytes, done); }
 
 // Compute units of the current device (256 when the runtime cannot say).
 inline int compute_units() {
@@ -722,7 +725,15 @@ fopd_status launch_mx4_raw(const unsigned char* w, int64_t V, const void* h, fop
 // (of 192 registers spill: 111 / 255); d = 512 128 x 50,000 15.5 / 12.5, d = 16,384 119 / 106.
 bool mx4_streams(int64_t T, int64_t V) { return T > 48 && T <= 160 && V > (T > 64 ? 192 : 256) * MxStream<4>::kVocabulary; }
 
-// weight [V, d] and hidden rows [T, d], both packed.
+// All kernels of tiles at the first call, whichever it takes: one call of any size before a capture is enough.
+fopd_status allow_mx4_tiles() {
+  static bool done[kMaxDevices] = {};
+  return allow_dynamic_lds({reinterpret_cast<const void*>(fopd_mx4_tiles<FOPD_BF16, false>), reinterpret_cast<const void*>(fopd_mx4_tiles<FOPD_BF16, true>),
+                            reinterpret_cast<const void*>(fopd_mx4_tiles<FOPD_F32, false>), reinterpret_cast<const void*>(fopd_mx4_tiles<FOPD_F32, true>)},
+                           kMxTileLds, done);
+}
+
+// weight [V, d] and hidden rows [T, d], both packed.  After allow_mx4_tiles.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
   const int64_t few = ((V + 63) / 64) * ((T + 63) / 64);    // workgroups of fopd_mx4_few
@@ -747,9 +758,6 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
     const bool walk = gemm_walks(static_cast<int64_t>(tiles_m) * tiles_n, Mx4Layout(V, d).steps, false);
     auto tiles = dt == FOPD_BF16 ? (walk ? fopd_mx4_tiles<FOPD_BF16, true> : fopd_mx4_tiles<FOPD_BF16, false>)
                                  : (walk ? fopd_mx4_tiles<FOPD_F32, true> : fopd_mx4_tiles<FOPD_F32, false>);
-    static bool done[2][2][kMaxDevices] = {};
-    const fopd_status st = allow_dynamic_lds(reinterpret_cast<const void*>(tiles), kMxTileLds, done[dt == FOPD_BF16][walk]);
-    if (st != FOPD_OK) return st;
     tiles<<<gemm_grid((tile_groups(tiles_m, tiles_n) + 7) / 8, walk), kLmThreads, kMxTileLds, s>>>(w, V, h, T, d, out, ldo, tiles_m, tiles_n);
     return launched();
   }
@@ -2066,6 +2074,7 @@ fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ld
   if (workspace == nullptr || misaligned(workspace, 256) || workspace_bytes < fopd_mx4_logits_workspace_bytes(T, V, d))
     return FOPD_EWORKSPACE;
   if (T == 0) return FOPD_OK;
+  if ((st = allow_mx4_tiles()) != FOPD_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (mx4_raw_rows(T, V)) return launch_mx4_raw(static_cast<const unsigned char*>(weight), V, hidden, dt_hidden, ldh, T, d, logits, dt, ld, s);
   unsigned char* packed = at<unsigned char>(workspace, 256);
