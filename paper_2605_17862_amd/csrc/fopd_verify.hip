@@ -318,7 +318,7 @@ fopd_verify_race(VerifyArgs a, int splits, const RowPart* __restrict__ parts, co
   constexpr int E = Elem<DT>::kPerVec;
   extern __shared__ __align__(16) unsigned char verify_smem[];
   RowPart* rows = reinterpret_cast<RowPart*>(verify_smem);             // [target, drafter][K + 1]
-  __shared__ int sh_kept, sh_next, sh_last;
+  __shared__ int sh_kept, sh_next, sh_last, sh_nothing;
   __shared__ RaceEntry sh_race[kVerifyThreads / 64];
   const unsigned nth = blockIdx.x / static_cast<unsigned>(pieces);
   const int i = a.B - 1 - static_cast<int>(nth), piece = static_cast<int>(blockIdx.x - nth * pieces);
@@ -503,9 +503,9 @@ fopd_verify_race(VerifyArgs a, int splits, const RowPart* __restrict__ parts, co
         best = key == 0 ? RaceEntry{-1.f, kNowhere} : RaceEntry{__uint_as_float(static_cast<uint32_t>(key >> 32)), static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key))};
       }
     }
-    if (tid == 0) sh_last = best.at == kNowhere;
+    if (tid == 0) sh_nothing = best.at == kNowhere;        // (not sh_last, which other wavefronts may still have to read)
     __syncthreads();
-    if (sh_last != 0) {                       // p nowhere above q, by rounding or because accept_u is 1: p itself
+    if (sh_nothing != 0) {                     // p nowhere above q, by rounding or because accept_u is 1: p itself
       best = RaceEntry{-1.f, kNowhere};
       enter(std::true_type(), std::false_type(), 0, nvec, true);
       reduce();

@@ -446,3 +446,23 @@ def test_smaller_batches_in_the_workspace_of_a_larger_one():
         b.ws = ws
         b.check(at_least=0.7 if B > 1 else 0.0)
     assert bool((guarded[n:] == 77).all())
+
+
+@pytest.mark.parametrize("V", [5000, 40001, 151936])
+@pytest.mark.parametrize("B", [1, 3, 70])
+def test_a_race_over_many_pieces_that_nobody_wins(B, V):
+    """The drafter is the target and the draft is refused all the same: the last workgroup races for the target's own row."""
+    b = Batch(B, 1, V, "f32", seed=43, away=0.0, taus=(0.8,))
+    b.draft[:, :V] = b.target[:, :V]
+    b.u[:] = 1.0
+    for _ in range(3):
+        b.outs()
+        b.run()
+        assert b.n.tolist() == [0] * B
+        z = b.target[::2, :V].double() / b.temperature.double()[:, None]
+        score = torch.log_softmax(z, 1) - b.noise[:, :V].double().log()
+        first, second = score.topk(2, dim=1).values.unbind(1)
+        sure = first - second > MARGIN
+        assert int(sure.sum()) >= 0.9 * B
+        assert torch.equal(b.out_ids[::2][sure].long(), score.argmax(dim=1)[sure])
+        assert b.out_mask.tolist() == B * [1, 0] and fb.fopd_workspace_status(b.ws) == (0, 0)
