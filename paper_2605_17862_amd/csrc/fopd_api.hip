@@ -850,13 +850,22 @@ fopd_status check_grad_tensor(const fopd_grad_tensor& t, bool with_out) {
   return FOPD_OK;
 }
 
-// launch(table) for the tensors of a list, kGradTable of them or kGradMaxPieces pieces at a time; with outputs from the last on.
+// launch(table) for the tensors of a list, kGradTable of them or kGradMaxPieces pieces at a time; with outputs the last ones first,
+// in a table in their order (fopd_grad_scale takes its pieces from the last one down).
 template <typename Launch>
 fopd_status grad_tables(const fopd_grad_tensor* tensors, int32_t n, bool with_out, Launch launch) {
   GradTable g;
   g.n = g.pieces = 0;
   auto flush = [&]() {
     if (g.n == 0) return FOPD_OK;
+    if (with_out) {                                        // (filled from the back)
+      std::reverse(g.t, g.t + g.n);
+      int32_t at = 0;
+      for (GradEntry* e = g.t; e != g.t + g.n; ++e) {
+        e->first_piece = at;
+        at += e->rows * e->row_pieces;
+      }
+    }
     const fopd_status st = launch(g);
     g.n = g.pieces = 0;
     return st;

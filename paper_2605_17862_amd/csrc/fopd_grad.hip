@@ -14,7 +14,8 @@
 // captured launch keeps its own table.  A tensor is rows of `cols` entries; rows that follow each other without a gap are one
 // long row.  It is cut into pieces of kGradPieceBytes of a row, dealt to the workgroups in turn; a lane has all 16-byte loads of a
 // piece in flight at once.  The norm goes through the list from the front, the scaling from the back: what the norm read
-// last is still in the Infinity Cache.
+// last is still in the Infinity Cache.  (The scaling's own traffic leaves that there: tensors from the front, each from its end, take
+// as long, 8 layers of width 4096 in bf16 646 us, so 648.)
 
 #ifndef FOPD_GRAD_HIP_
 #define FOPD_GRAD_HIP_

@@ -24,3 +24,45 @@ def test_one_product_of_any_size_prepares_all_its_kernels(tmp_path):
     assert [n for _, n, _ in calls] == sorted({n for _, n, _ in calls})      # each launched something
     assert calls[0][2] > 0 and all(n == calls[0][2] for _, _, n in calls), calls
     assert kernels == 8                                      # (packing, few rows as they are and packed, some rows, all four of tiles)
+
+
+def test_scaling_goes_through_the_list_from_its_end(tmp_path):
+    """fopd_grad_norm reads the tensors in order and leaves the last ones in the cache; fopd_grad_scale takes a table's pieces from
+    the last one down, so tables hold the list's order and come from its end."""
+    got = recorded(tmp_path, """
+        class Entry(Structure):
+            _fields_ = [("grad", c_int64), ("out", c_int64), ("cols", c_int64), ("ld", c_int64), ("ld_out", c_int64), ("rows", c_int32),
+                        ("row_pieces", c_int32), ("first_piece", c_int32), ("bf16", c_int8), ("out_bf16", c_int8)]
+        class Table(Structure):
+            _fields_ = [("n", c_int32), ("pieces", c_int32), ("t", Entry * 48)]
+        class Tensor(Structure):
+            _fields_ = [("grad", c_int64), ("out", c_int64), ("rows", c_int64), ("cols", c_int64), ("ld", c_int64), ("ld_out", c_int64),
+                        ("dt", c_int), ("dt_out", c_int)]
+        lib.fopd_grad_norm.argtypes = [P, c_int32, c_int, P, P, P, c_size_t, P]
+        lib.fopd_grad_clip.argtypes = [P, c_int32, P, c_float, c_float, P, P]
+        c_int.in_dll(rec, "argument_bytes").value = sizeof(Table)
+        result = []
+        for n in (1, 2, 41, 48, 49, 130):
+            # one piece, several, rows with gaps and nothing at all, at addresses that count up
+            shapes = [[(3, 5, 5), (1, 30000, 30000), (7, 100, 104), (0, 5, 5)][(i + 1) % 4] for i in range(n)]
+            ts = (Tensor * n)(*[Tensor(1 << 20 | i << 8, 1 << 20 | i << 8, r, c, ld, ld, i % 2, i % 2) for i, (r, c, ld) in enumerate(shapes)])
+            begin = count("launches")
+            assert lib.fopd_grad_norm(ts, n, 0, P(4096), None, P(4096), 1 << 20, None) == 0
+            middle = count("launches")
+            assert lib.fopd_grad_clip(ts, n, P(4096), 1.0, 0.0, None, None) == 0
+            raw = (c_char * 4096 * count("launches")).in_dll(rec, "arguments")
+            tables = [Table.from_buffer_copy(raw[k][:sizeof(Table)].ljust(sizeof(Table), bytes(1))) for k in range(begin, count("launches"))]
+            told = [[g.pieces, [[e.grad >> 8 & 4095, e.first_piece, e.rows * e.row_pieces] for e in g.t[:g.n]]] for g in tables]
+            result.append([n, told[:middle - begin], told[middle - begin:]])
+    """)
+    for n, norm, scale in got:
+        present = [i for i in range(n) if (i + 1) % 4 != 3]
+        for pieces, entries in norm + scale:
+            at = 0
+            for _, first, count in entries:
+                assert first == at
+                at += count
+            assert at == pieces
+        assert [e[0] for _, entries in norm for e in entries] == present
+        assert len(scale) == (len(present) + 47) // 48
+        assert [e[0] for _, entries in reversed(scale) for e in entries] == present, (n, scale)
