@@ -181,9 +181,12 @@ inline P* at(void* ws, size_t off) {
 
 inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
 
+// Of a row: the kernels form the places behind its last vector, one a lane, in 32 bits, up to 512 lanes of them.
+constexpr int64_t kMaxColumns = (1LL << 31) - 512;
+
 fopd_status check_matrix(const void* m, fopd_dtype dt, int64_t T, int64_t V, int64_t ld) {
   if (dt != FOPD_F32 && dt != FOPD_BF16) return FOPD_EDTYPE;
-  if (T < 0 || T > 2147483647LL || V <= 0 || ld < V || V > 2147483647LL - 16) return FOPD_ESHAPE;
+  if (T < 0 || T > 2147483647LL || V <= 0 || ld < V || V > kMaxColumns) return FOPD_ESHAPE;
   if (m == nullptr) return FOPD_EINVAL;
   const size_t es = (dt == FOPD_F32) ? 4 : 2;
   if (misaligned(m, 16) || (static_cast<size_t>(ld) * es) % 16 != 0) return FOPD_EALIGN;

@@ -466,3 +466,26 @@ def test_a_race_over_many_pieces_that_nobody_wins(B, V):
         assert int(sure.sum()) >= 0.9 * B
         assert torch.equal(b.out_ids[::2][sure].long(), score.argmax(dim=1)[sure])
         assert b.out_mask.tolist() == B * [1, 0] and fb.fopd_workspace_status(b.ws) == (0, 0)
+
+
+def test_the_largest_vocabulary():
+    """2^31 - 512 entries, whose last places are as far as 32 bits go."""
+    V = (1 << 31) - 512 - 3                                                # (entries behind the last whole vector)
+    ld = (V + 7) // 8 * 8
+    target = torch.full((1, ld), float("-inf"), dtype=torch.bfloat16, device=DEV)
+    places = [0, 12345, (1 << 30) + 1, V - 300, V - 2, V - 1]
+    z = [1.0, 2.0, 0.5, 1.5, 2.5, 1.0]
+    target[0, places] = torch.tensor(z, dtype=torch.bfloat16, device=DEV)
+    noise = torch.ones(1, ld, device=DEV)
+    n, ids = (torch.full((1,), -9, dtype=torch.int32, device=DEV) for _ in range(2))
+    logp, mask = torch.full((1,), 9.0, device=DEV), torch.full((1,), 9, dtype=torch.uint8, device=DEV)
+    ws = _workspace(fb.fopd_verify_workspace_bytes(1, V, 1))
+    p = np.exp(z) / np.exp(z).sum()
+    for first in range(len(places)):                                       # each of them wins once
+        noise[0, places] = 1.0
+        noise[0, places[first]] = 0.01
+        fb.fopd_verify_draft(target, None, fb.FOPD_BF16, 1, V, ld, ld, None, None, None, 1, 0, None, None, noise, ld, n, ids, logp, mask, ws)
+        assert (int(n), int(ids), int(mask)) == (0, places[first], 1)
+        assert abs(float(logp) - math.log(p[first])) <= 2.0 ** -20         # (six terms)
+    fb.fopd_verify_draft(target, None, fb.FOPD_BF16, 1, V, ld, ld, None, None, None, 1, 0, None, None, None, 0, n, ids, logp, mask, ws)
+    assert int(ids) == V - 2 and fb.fopd_workspace_status(ws) == (0, 0)

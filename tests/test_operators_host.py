@@ -118,6 +118,18 @@ def test_a_workspace_for_a_verification_serves_every_smaller_one(V):
     assert max(fb.fopd_verify_workspace_bytes(8 * B, V, B) for B in range(1, 257)) == fb.fopd_verify_workspace_bytes(2048, V, 256)
 
 
+def test_rows_whose_last_places_do_not_fit_32_bits_are_refused():
+    """A workgroup forms the places behind a row's last vector, as many as it has lanes: they have to stay below 2^31."""
+    lib = fb.load_library()
+    most = (1 << 31) - 512
+    for V in ((1 << 31) - 17, (1 << 31) - 256, most + 1):
+        assert _verify(lib, V=V, ld=1 << 31, ldd=1 << 31, lde=1 << 31) == 2
+        assert lib.fopd_token_logprobs(P(4096), 1, 1, V, 1 << 31, P(4096), None, P(4096), P(4096), None, None, P(4096), 0, None) == 2
+        assert lib.fopd_mx4_dequantize(P(4096), 1 << 40, 1, V, P(4096), 1, 1 << 31, None) == 2
+    assert _verify(lib, V=most, ld=1 << 31, ldd=1 << 31, lde=1 << 31, ws=None) == 5
+    assert lib.fopd_token_logprobs(P(4096), 1, 1, most, 1 << 31, P(4096), None, P(4096), P(4096), None, None, P(4096), 0, None) == 5
+
+
 def test_status_of_a_row_without_a_distribution():
     assert fb.fopd_flags_status(16) == 12
     assert fb.fopd_flags_status(17) == 6
