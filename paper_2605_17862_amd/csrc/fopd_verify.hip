@@ -89,7 +89,8 @@ __device__ __forceinline__ VerifySample verify_sample(const VerifyArgs& a, int i
   s.there = s.len >= 0 && s.len <= a.K && s.row >= 0 && s.row <= a.rows - 1 - s.len;
   const float tau = a.temperature != nullptr ? a.temperature[i] : 1.f;
   s.greedy = a.noise == nullptr || tau == 0.f;
-  s.c = s.greedy ? kLog2e : (tau > 0.f && tau < __builtin_inff() ? kLog2e / tau : __builtin_nanf(""));
+  // (a temperature whose inverse is past the type's range is as good as one that is not: entries differ, or they do not)
+  s.c = s.greedy ? kLog2e : (tau > 0.f && tau < __builtin_inff() ? fminf(kLog2e / tau, __FLT_MAX__) : __builtin_nanf(""));
   return s;
 }
 

@@ -489,3 +489,19 @@ def test_the_largest_vocabulary():
         assert abs(float(logp) - math.log(p[first])) <= 2.0 ** -20         # (six terms)
     fb.fopd_verify_draft(target, None, fb.FOPD_BF16, 1, V, ld, ld, None, None, None, 1, 0, None, None, None, 0, n, ids, logp, mask, ws)
     assert int(ids) == V - 2 and fb.fopd_workspace_status(ws) == (0, 0)
+
+
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("tau", [1.0, 1e-20, 1e-37, 5e-39, 4e-39, 1e-42, 2.0 ** -149])
+def test_the_smallest_temperatures_leave_the_largest_entries(tau, draft):
+    """From some size down p is 1 / n at the n largest entries and 0 elsewhere; the temperature's inverse need not be a number of the type."""
+    b = Batch(12, 2, 5003, "f32", seed=44, draft=draft, taus=(tau,))
+    z = torch.round(b.target[:, :5003] * 2.0)
+    b.target[:, :5003] = z
+    b.target[4, :5003] -= z[4].max()                                       # (a largest entry of 0)
+    if draft:
+        b.draft[:, :5003] = z + torch.round(torch.randn(z.shape, generator=torch.Generator().manual_seed(2)).to(DEV) * 0.6)
+    b.ids = z.argmax(dim=1).to(torch.int32)
+    b.ids[::5] = 7
+    b.run()
+    b.check(at_least=0.9)
