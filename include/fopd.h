@@ -689,7 +689,8 @@ fopd_status fopd_verify_draft(const void* target_logits, const void* draft_logit
  *                  With accumulate != 0 the sum is added to what sum_sq holds: lists that do not fit one call; with gradients
  *                  sharded over ranks, sum_sq of the ranks are added up by the caller between the two calls.
  * fopd_grad_clip   out = c grad,  c = min(1, max_norm / (sqrt(sum_sq[0]) + eps)), rounded to f32; coef[0] = c (may be NULL).  The
- *                  product is rounded once to out's type.  A tensor clipped in place with c = 1 is left as it is.
+ *                  product is rounded once to out's type.  A tensor clipped in place with c = 1 is left as it is.  c = 1 where the norm
+ *                  and eps are both 0, max_norm = 0 too.
  *                  A norm that is NaN or infinite makes c NaN or 0, and the results accordingly.
  * A tensor is `rows` rows of `cols` entries, row r at grad + r ld; out likewise with ld_out, of the same shape.  Only the alignment of
  * the element type is needed (16 bytes are faster).  out == grad (then of the same type and pitch) clips in place; else

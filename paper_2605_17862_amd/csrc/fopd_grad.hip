@@ -197,7 +197,9 @@ fopd_grad_sum_squares(GradTable g, double* partial, int first_cached, GradFinish
 
 // c < 1 or NaN as it is, else 1: a norm that is no number makes every entry one.
 __device__ __forceinline__ float grad_coefficient(double sum_sq, float max_norm, float eps) {
-  const double c = static_cast<double>(max_norm) / (sqrt(sum_sq) + static_cast<double>(eps));
+  const double norm = sqrt(sum_sq) + static_cast<double>(eps);
+  if (norm == 0.0) return 1.f;                             // nothing but zeros, whatever max_norm
+  const double c = static_cast<double>(max_norm) / norm;
   return static_cast<float>(c >= 1.0 ? 1.0 : c);
 }
 

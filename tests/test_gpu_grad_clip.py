@@ -206,3 +206,29 @@ def test_entries_past_32_bit_offsets():
     assert float(norm) == 5.0
     fb.fopd_grad_clip(tensors, sum_sq, 2.5, 0.0, coef)
     assert float(g[3]) == 1.5 and float(g[-2]) == 2.0 and float(g[-1]) == 0.0
+
+
+@pytest.mark.parametrize("most", [0.0, 1.0, float("inf")])
+@pytest.mark.parametrize("place", ["in_place", "out"])
+def test_zero_gradients_stay_zero_for_any_bound(most, place):
+    grads = [torch.zeros(5000, device=DEV), torch.zeros(3, dtype=torch.bfloat16, device=DEV)]
+    outs = grads if place == "in_place" else [torch.full_like(g, 7.0) for g in grads]
+    tensors = fb.grad_tensors(grads, outs)
+    for eps in (0.0, EPS):
+        sum_sq, norm, coef = _scalars()
+        fb.fopd_grad_norm(tensors, sum_sq, norm, _ws())
+        fb.fopd_grad_clip(tensors, sum_sq, most, eps, coef)
+        assert float(norm) == 0.0 and float(coef) == oo.grad_clip([_f64(g) for g in grads], most, eps)[2]
+        assert all(bool((o == 0.0).all()) for o in outs)
+
+
+def test_a_bound_of_zero_and_none_at_all():
+    grads = [torch.randn(5000, generator=torch.Generator().manual_seed(1)).to(DEV)]
+    outs = [torch.full_like(grads[0], 7.0)]
+    tensors = fb.grad_tensors(grads, outs)
+    sum_sq, norm, coef = _scalars()
+    fb.fopd_grad_norm(tensors, sum_sq, norm, _ws())
+    fb.fopd_grad_clip(tensors, sum_sq, 0.0, 0.0, coef)
+    assert float(coef) == 0.0 and bool((outs[0] == 0.0).all())
+    fb.fopd_grad_clip(tensors, sum_sq, float("inf"), 0.0, coef)
+    assert float(coef) == 1.0 and torch.equal(outs[0], grads[0])
