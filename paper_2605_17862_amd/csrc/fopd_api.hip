@@ -840,12 +840,14 @@ constexpr int kGradPartials = 1 << 14;
 // two (4 / 8 / 16: + 0.5 % / 0 / - 1 %; of 32 M entries 64.4 / 66.0 / 69.2 us).
 constexpr int kGradSumGrid = 512, kGradScaleGrid = 2048;
 
+constexpr int64_t kGradMaxEntries = 1LL << 40;             // of a tensor
+static_assert(kGradMaxEntries / (kGradPieceBytes / 4) <= kGradMaxPieces, "a row's pieces fit a launch");
+
 fopd_status check_grad_tensor(const fopd_grad_tensor& t, bool with_out) {
   if ((t.dt != FOPD_F32 && t.dt != FOPD_BF16) || (with_out && t.dt_out != FOPD_F32 && t.dt_out != FOPD_BF16)) return FOPD_EDTYPE;
-  constexpr int64_t kMost = 1LL << 40;
   if (t.rows < 0 || t.cols < 0) return FOPD_ESHAPE;
   if (t.rows == 0 || t.cols == 0) return FOPD_OK;
-  if (t.rows > kMost / t.cols) return FOPD_ESHAPE;
+  if (t.rows > kGradMaxEntries / t.cols) return FOPD_ESHAPE;
   if (t.rows > 1 && (t.ld < t.cols || (with_out && t.ld_out < t.cols))) return FOPD_ESHAPE;
   if (t.grad == nullptr || (with_out && t.out == nullptr)) return FOPD_EINVAL;
   if (with_out && t.out == t.grad && (t.dt != t.dt_out || (t.rows > 1 && t.ld != t.ld_out))) return FOPD_EINVAL;
@@ -882,9 +884,8 @@ fopd_status grad_tables(const fopd_grad_tensor* tensors, int32_t n, bool with_ou
       rows = 1;
     }
     const int64_t piece = kGradPieceBytes >> (t.dt == FOPD_BF16 ? 1 : 2), row_pieces = (cols + piece - 1) / piece;
-    if (row_pieces > kGradMaxPieces) return FOPD_ESHAPE;
     for (int64_t r = 0; r < rows;) {
-      const int64_t here = std::min(rows - r, std::max<int64_t>(1, kGradMaxPieces / row_pieces));
+      const int64_t here = std::min(rows - r, kGradMaxPieces / row_pieces);
       if (g.n == kGradTable || g.pieces + here * row_pieces > kGradMaxPieces) {
         const fopd_status st = flush();
         if (st != FOPD_OK) return st;

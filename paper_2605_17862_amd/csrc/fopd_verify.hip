@@ -177,13 +177,6 @@ __device__ __forceinline__ double verify_probability(const RowPart& p, float c, 
   return exp2((static_cast<double>(z) - static_cast<double>(p.top)) * static_cast<double>(c)) / (1.0 + static_cast<double>(p.others));
 }
 
-__device__ __forceinline__ void race_merge(float& s, int& at, float s2, int at2) {
-  if (s2 > s || (s2 == s && at2 < at)) {
-    s = s2;
-    at = at2;
-  }
-}
-
 }  // namespace
 
 // Workgroup ((sample, tensor) (K + 1) + row) splits + piece, the tensors of a sample one after the other; parts[(tensor R + row of
