@@ -505,3 +505,18 @@ def test_the_smallest_temperatures_leave_the_largest_entries(tau, draft):
     b.ids[::5] = 7
     b.run()
     b.check(at_least=0.9)
+
+
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("tau", [-1.0, -1e-45, float("nan"), float("inf"), float("-inf")])
+def test_a_temperature_that_is_none_ends_its_sample_before_the_first_row(tau, draft):
+    b = Batch(3, 2, 90, "f32", seed=45, draft=draft, away=0.0)
+    b.u.fill_(0.0)
+    b.taus = torch.tensor([1.0, tau, 1.0])
+    b.temperature = b.taus.to(DEV)
+    b.run()
+    assert b.n.tolist() == [2, 0, 2] and fb.fopd_workspace_status(b.ws) == (12, 16)
+    ids, logp, mask = b.out_ids.view(3, 3), b.out_logp.view(3, 3), b.out_mask.view(3, 3)
+    assert ids[1].tolist() == [-1, -1, -1] and mask.tolist() == [[1, 1, 1], [0, 0, 0], [1, 1, 1]]
+    assert math.isnan(float(logp[1, 0])) and logp[1, 1:].tolist() == [0.0, 0.0]
+    assert bool(torch.isfinite(logp[[0, 2]]).all()) and torch.equal(ids[[0, 2], :2], b.ids.view(3, 3)[[0, 2], :2])
