@@ -667,6 +667,10 @@ fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ld
  *   workspace      fopd_verify_workspace_bytes(R, V, B) bytes, 256-byte aligned, initialised once with fopd_workspace_init; it serves
  *                  any call with at most R rows, V entries and B samples
  *
+ * out_logp is at the temperature that the token was drawn at, log-probs that the loss forms are at 1: with out_logp of other
+ * temperatures as behav_logp a sample drifts at lag 0 already.  fopd_token_logprobs over target_logits with out_ids and out_mask
+ * gives them at 1.  A cut of the distribution (top-p, top-k) is the caller's, -inf in both logits tensors before the call.
+ *
  * On the device: draft_lens outside 0 .. max_draft or rows outside [0, R) raise FOPD_ESEGMENTS, n_accepted is 0 and no row is
  * written (in a padded batch: -1, 0, 0).  A drafted id outside [0, V) raises FOPD_ETOKEN_RANGE and is not kept.  A row that is
  * reached and is no distribution (no finite entry, NaN, +inf; or tau_i negative, NaN or infinite) raises FOPD_EDIST; the sample ends before it

@@ -520,3 +520,34 @@ def test_a_temperature_that_is_none_ends_its_sample_before_the_first_row(tau, dr
     assert ids[1].tolist() == [-1, -1, -1] and mask.tolist() == [[1, 1, 1], [0, 0, 0], [1, 1, 1]]
     assert math.isnan(float(logp[1, 0])) and logp[1, 1:].tolist() == [0.0, 0.0]
     assert bool(torch.isfinite(logp[[0, 2]]).all()) and torch.equal(ids[[0, 2], :2], b.ids.view(3, 3)[[0, 2], :2])
+
+
+def test_verified_rollouts_and_the_loss_at_other_temperatures_than_one():
+    """Verification gives log-probs at the sampling temperature; the loss forms its own at 1.  With behaviour log-probs at 1, from
+    fopd_token_logprobs over the verified rows, a fresh sample (lag 0) has no drift."""
+    B, K, V = 8, 3, 1500
+    b = Batch(B, K, V, "bf16", seed=46, taus=(0.6, 0.7))
+    b.run()
+    b.check()
+    T = b.R
+    lens, lag = torch.full((B,), K + 1, dtype=torch.int32, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+    loss_ws = _workspace(fb.fopd_workspace_bytes(T, B))
+    at_one, lse = torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+    fb.fopd_token_logprobs(b.target, b.dt, T, V, b.ld, b.out_ids, b.out_mask, at_one, lse, None, None, loss_ws)
+    kept = b.out_mask.bool()
+    z = b.target[:, :V].double()
+    want = torch.log_softmax(z, 1).gather(1, b.out_ids.long().clamp(min=0)[:, None])[:, 0]
+    assert float((at_one.double() - want)[kept].abs().max()) <= 1e-4
+    assert float((b.out_logp.double() - want)[kept].abs().max()) > 1e-2   # (the two temperatures differ)
+    teacher = (at_one - 0.3).contiguous()
+    drift = {}
+    for name, behav in (("at one", at_one), ("sampled", b.out_logp)):
+        out = [torch.empty(B, dtype=dt, device=DEV) for dt in (torch.int32, torch.int32) + 6 * (torch.float32,)]
+        agg, cu = torch.empty(3, device=DEV), torch.empty(B + 1, dtype=torch.int64, device=DEV)
+        n_train, n_roll, d_roll, d_sup, ell, cover, cover_roll, fresh = out
+        fb.fopd_freshness_score(at_one, behav, None, None, teacher, None, b.out_mask, lens, lag, T, B, (1.0, 1.0, 0.05, 0.1), cu,
+                                n_train, n_roll, d_roll, d_sup, ell, cover, cover_roll, fresh, agg, loss_ws)
+        drift[name] = d_roll.clone()
+        assert n_train.tolist() == (b.n + 1).tolist()
+    assert fb.fopd_workspace_status(loss_ws) == (0, 0)
+    assert bool((drift["at one"] == 0.0).all()) and bool((drift["sampled"] != 0.0).all())
