@@ -689,9 +689,17 @@ fopd_status launch_mx4_pack(const void* in, fopd_dtype dt, int64_t R, int64_t d,
 // 32,000 16.1 / 19.6, 70,000 (two weights in turn, 305 MB) 34.1 / 31.0, 100,000 47.0 / 41.3; one row x 151,936 61.2 / 54.1.
 constexpr int64_t kMxCachedBytes = 128LL << 20;
 // Blocks of 64 x 64 results up to which fopd_mx4_few is the faster one, whose workgroups spread over the chip where there are few tiles of 256 x
-// 256; with more of them the weight is read too often.  Blocks / it / tiles, us: d = 4096 256 12.3 / 31.9, 512 16.1 / 34.0, 1000 29.0 / 34.1, 1024
-// 25.9 / 38.4, 1500 42.1 / 38.2, 1408 34.8 / 38.5, 2000 53.1 / 38.5, 2048 44.9 / 39.6; d = 1024 1000 15.9 / 25.0; d = 512 2504 24.5 / 16.1.
-constexpr int64_t kMxFewGroups = 1280;
+// 256; with more of them the weight is read too often.  Workgroups go to the eight XCDs in turn, so with a multiple of four blocks along
+// the vocabulary those that read the same weight meet in one or two L2s, and more blocks pay, unless there are only three groups of rows to share
+// it.  Rows x V (blocks), it / tiles, us, d = 4096: 192 x 21,824 (1023) 29.8 / 34.4, 192 x 27,264 (1278) 37.5 / 34.6, 192 x 32,768 (1536) 41.2 / 35.1,
+// 256 x 16,384 (1024) 24.4 / 35.5, 256 x 17,600 (1100, 275 along V) 36.8 / 35.8, 256 x 22,528 (1408) 35.3 / 35.6, 448 x 11,648 (1274, 182 along V) 38.2 / 35.4, 512 x
+// 11,264 (1408) 30.7 / 35.6, 512 x 13,568 (1696) 44.9 / 36.1, 1024 x 4352 (1088, 68 along V) 30.6 / 37.3, 1024 x 4800 (1200, 75 along V) 39.4 / 37.3, 1024 x 5632 (1408) 31.8 /
+// 36.0.  The borders move little with d: 256 x 16,384 / 17,600 / 22,528 13.3 / 17.2, 17.4 / 17.3, 16.7 / 17.1 with 1024, 38.7 / 61.0 for the first with 8192.
+constexpr int64_t kMxFewBlocks = 1024, kMxFewSharedBlocks = 1408;
+bool mx4_few_blocks(int64_t T, int64_t V) {
+  const int64_t along_v = (V + 63) / 64, blocks = along_v * ((T + 63) / 64);
+  return T <= 64 || blocks <= kMxFewBlocks || (T > 192 && along_v % 4 == 0 && blocks <= kMxFewSharedBlocks);
+}
 constexpr int64_t kMxMaxVocabulary = 1LL << 28;           // (a launch has at most 2^32 lanes)
 
 // launch(type, whether the weight is read by ordinary loads), both as types.
@@ -705,9 +713,9 @@ fopd_status mx4_variant(fopd_dtype dt, bool cached, Launch launch) {
 
 // Few hidden rows are quantised by the workgroups that use them, each for itself, and the launch that packs them falls away; with many
 // results the workgroups, each of which reads all rows again, take longer than that launch.  Rows x V, d = 4096, quantised by the workgroups /
-// packed first, us: 1 x 4096 7.7 / 10.4, 16 x 8192 10.7 / 11.1, 8 x 16384 12.6 / 11.9, 16 x 16384 13.1 / 12.0, 4 x 32000 14.6 / 15.3, 16 x 32000
-// 17.8 / 15.5, 2 x 64000 24.7 / 25.0, 8 x 64000 28.6 / 25.4, 1 / 2 / 4 / 16 x 151,936 52.7 / 52.9 / 55.1 / 82.0 and 53.8 / 53.9 / 54.4 / 57.4;
-// d = 1024 16 x 16384 7.6 / 10.3.
+// packed first, us: 1 x 4096 7.7 / 9.8, 16 x 8192 9.5 / 9.6, 8 x 16,384 10.4 / 11.1, 4 x 32,000 13.9 / 14.8, 16 x 16,384 11.2 / 11.2, 4 x 64,000 23.8 / 23.6, 16 x
+// 32,000 17.3 / 15.1, 8 x 64,000 26.9 / 23.9, 1 / 2 / 4 / 16 x 151,936 50.8 / 51.3 / 53.2 / 80.5 and 52.2 / 52.3 / 52.9 / 56.4;
+// d = 1024 16 x 16,384 6.9 / 9.6, 16 x 151,936 18.1 / 17.3.
 bool mx4_raw_rows(int64_t T, int64_t V) { return T <= 2 || (T <= 16 && T * V <= 1 << 17); }
 
 // weight [V, d] packed, the few hidden rows as they are.
@@ -722,11 +730,14 @@ fopd_status launch_mx4_raw(const unsigned char* w, int64_t V, const void* h, fop
   });
 }
 
-// Rows for fopd_mx4_stream, and workgroups of it for most compute units.  The kernel taken without this rule / it, us, d = 4096: 45 x 151,936
-// 65.1 / 65.7; 64 x 32,000 / 40,000 / 151,936 17.8 / 21.0, 24.9 / 21.6, 75.6 / 69.0; 96 x 24,000 / 40,000 / 151,936 26.3 / 24.6, 37.1 / 25.7, 105 /
-// 78.8; 128 x 16,384 / 24,000 / 151,936 15.8 / 27.8, 26.5 / 25.9, 111 / 81.5; 160 x 24,000 / 65,536 / 151,936 37.0 / 29.2, 39.2 / 41.0, 111 / 91.1
-// (of 192 registers spill: 111 / 255); d = 512 128 x 50,000 15.5 / 12.5, d = 16,384 119 / 106.
-bool mx4_streams(int64_t T, int64_t V) { return T > 48 && T <= 160 && V > (T > 64 ? 192 : 256) * MxStream<4>::kVocabulary; }
+// Rows for fopd_mx4_stream, and blocks of 64 x 64 past which fopd_mx4_few goes through the chip once or twice more.  The kernel taken without this rule /
+// it, us, d = 4096: 64 x 32,000 / 40,000 / 151,936 17.4 / 19.9, 24.4 / 21.3, 74.8 / 68.6; 96 x 16,384 / 17,000 / 24,000 / 151,936 14.6 / 20.8, 24.1 / 21.9, 25.9 / 22.6,
+// 105 / 79.5; 128 x 16,384 / 17,000 / 21,504 / 24,000 / 151,936 14.7 / 22.7, 24.2 / 23.6, 22.7 / 24.2, 26.1 / 24.4, 115 / 81.2; 160 x 21,504 / 22,000 / 24,000 / 65,536 / 151,936 25.1 / 27.4,
+// 30.2 / 27.9, 36.1 / 27.5, 38.5 / 40.2 (256 tiles, the chip once), 112 / 91.5 (of 192 registers spill: 111 / 255).  d = 1024: 96 x 17,000 11.8 / 11.3, 160 x
+// 22,000 15.2 / 13.6, 128 x 151,936 42.7 / 30.7.  Up to 48 rows fopd_mx4_few is as fast: 45 x 151,936 65.1 / 65.7.
+bool mx4_streams(int64_t T, int64_t V) {
+  return T > 48 && T <= 160 && ((V + 63) / 64) * ((T + 63) / 64) > (T > 128 ? 1024 : 512);
+}
 
 // All kernels of tiles at the first call, whichever it takes: one call of any size before a capture is enough.
 fopd_status allow_mx4_tiles() {
@@ -739,7 +750,6 @@ fopd_status allow_mx4_tiles() {
 // weight [V, d] and hidden rows [T, d], both packed.  After allow_mx4_tiles.
 fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned char* h, int64_t T, int64_t d, void* out,
                                fopd_dtype dt, int64_t ldo, hipStream_t s) {
-  const int64_t few = ((V + 63) / 64) * ((T + 63) / 64);    // workgroups of fopd_mx4_few
   if (mx4_streams(T, V)) {
     return mx4_variant(dt, Mx4Layout(V, d).total <= kMxCachedBytes, [&](auto dt_tag, auto cached_tag) {
       constexpr int DT = decltype(dt_tag)::value;
@@ -756,7 +766,7 @@ fopd_status launch_mx4_product(const unsigned char* w, int64_t V, const unsigned
       return go(std::integral_constant<int, 10>());
     });
   }
-  if (T > 64 && few > kMxFewGroups) {
+  if (!mx4_few_blocks(T, V)) {
     const int tiles_m = static_cast<int>((V + kGemmTile - 1) / kGemmTile), tiles_n = static_cast<int>((T + kGemmTile - 1) / kGemmTile);
     const bool walk = gemm_walks(static_cast<int64_t>(tiles_m) * tiles_n, Mx4Layout(V, d).steps, false);
     auto tiles = dt == FOPD_BF16 ? (walk ? fopd_mx4_tiles<FOPD_BF16, true> : fopd_mx4_tiles<FOPD_BF16, false>)

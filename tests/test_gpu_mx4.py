@@ -264,3 +264,11 @@ def test_some_rows_that_are_nan_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert np.array_equal(z.cpu().numpy(), want.cpu().numpy(), equal_nan=True)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,d", [(65, 16385, 300), (96, 17003, 513), (128, 16450, 257), (129, 21889, 96), (160, 22001, 520), (128, 16384, 200), (160, 21800, 257),
+                                   (192, 27001, 130), (224, 22528, 300), (225, 22600, 300), (1024, 5632, 257), (1000, 5600, 96), (1030, 5888, 64)])
+def test_product_either_side_of_the_kernels_borders(T, V, d, kind):
+    z, hx, wx, _ = _logits(T, V, d, "bf16", kind, seed=T + V + d)
+    _check(z, hx, wx, T, V, d, kind)

@@ -66,3 +66,28 @@ def test_scaling_goes_through_the_list_from_its_end(tmp_path):
         assert [e[0] for _, entries in norm for e in entries] == present
         assert len(scale) == (len(present) + 47) // 48
         assert [e[0] for _, entries in reversed(scale) for e in entries] == present, (n, scale)
+
+
+def test_products_take_the_kernel_that_measured_fastest(tmp_path):
+    """Either side of each border between the kernels of few rows, of some and of tiles, told from each other by their workgroups."""
+    cases = {"few": [(49, 32000), (64, 32768), (96, 16384), (128, 16384), (129, 21504), (160, 21824), (161, 21824), (192, 21824), (256, 16384), (256, 22528),
+                     (512, 11264), (1024, 4352), (1024, 5632), (4096, 1024)],
+             "stream": [(49, 32769), (64, 40000), (65, 16385), (96, 24000), (128, 24000), (129, 21889), (160, 24000), (160, 151936)],
+             "tiles": [(161, 21889), (192, 27264), (192, 25600), (256, 17600), (256, 22592), (448, 11648), (512, 13568), (1024, 4800), (1024, 5888), (4096, 151936)]}
+    got = recorded(tmp_path, """
+        lib.fopd_mx4_bytes.restype = lib.fopd_mx4_logits_workspace_bytes.restype = c_size_t
+        lib.fopd_mx4_bytes.argtypes, lib.fopd_mx4_logits_workspace_bytes.argtypes = 2 * [c_int64], 3 * [c_int64]
+        lib.fopd_mx4_logits.argtypes = [P, c_int, c_int64, P, c_size_t, c_int64, c_int64, c_int64, P, c_int, c_int64, P, c_size_t, P]
+        result = {}
+        for name, sizes in CASES.items():
+            for T, V in sizes:
+                before, d = count("launches"), 4096
+                assert lib.fopd_mx4_logits(P(4096), 1, d, P(4096), lib.fopd_mx4_bytes(V, d), T, V, d, P(4096), 1, (V + 7) // 8 * 8, P(4096),
+                                           lib.fopd_mx4_logits_workspace_bytes(T, V, d), None) == 0
+                assert count("launches") == before + 2                     # the rows' packing, then the product
+                grid = (c_uint * count("launches")).in_dll(rec, "grids")[before + 1]
+                kind = {(V + 63) // 64: "few", (V + 127) // 128: "stream"}.get(grid, "tiles")
+                result["%s %d %d" % (name, T, V)] = kind
+    """.replace("CASES", repr(cases)))
+    assert len(got) == sum(map(len, cases.values()))
+    assert not {k: v for k, v in got.items() if k.split()[0] != v}
