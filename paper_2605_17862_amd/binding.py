@@ -568,22 +568,39 @@ def fopd_profile_read(which):
     return float(ms.value), int(n.value)
 
 
+_types = None
+
+
+def _matrix(x, dt, name):
+    """_ptr of a tensor of the type that `dt` names (read as another, a call would run past its end)."""
+    global _types
+    if _types is None:
+        import torch
+        _types = {FOPD_F32: torch.float32, FOPD_BF16: torch.bfloat16}
+    return _ptr(x, _types.get(int(dt)), name)
+
+
+def _packed(x, name):
+    """Address and bytes of a packed matrix: a tensor in device memory, or (address, bytes)."""
+    if not isinstance(x, tuple):
+        _ptr(x, None, name)
+    return _ws(x)
+
+
 def fopd_mx4_bytes(R, d):
     return int(load_library().fopd_mx4_bytes(int(R), int(d)))
 
 
 def fopd_mx4_quantize(x, dt, R, d, ld, packed, stream=None):
-    import torch
-    p, n = _ws(packed)
-    _check(load_library().fopd_mx4_quantize(_ptr(x, (torch.float32, torch.bfloat16), "x"), int(dt), int(R), int(d), int(ld),
+    p, n = _packed(packed, "packed")
+    _check(load_library().fopd_mx4_quantize(_matrix(x, dt, "x"), int(dt), int(R), int(d), int(ld),
                                             p, n, _stream(stream)), "fopd_mx4_quantize")
 
 
 def fopd_mx4_dequantize(packed, R, d, out, dt, ldo, stream=None):
-    import torch
-    p, n = _ws(packed)
-    _check(load_library().fopd_mx4_dequantize(p, n, int(R), int(d), _ptr(out, (torch.float32, torch.bfloat16), "out"), int(dt),
-                                              int(ldo), _stream(stream)), "fopd_mx4_dequantize")
+    p, n = _packed(packed, "packed")
+    _check(load_library().fopd_mx4_dequantize(p, n, int(R), int(d), _matrix(out, dt, "out"), int(dt), int(ldo), _stream(stream)),
+           "fopd_mx4_dequantize")
 
 
 def fopd_mx4_logits_workspace_bytes(T, V, d):
@@ -592,12 +609,10 @@ def fopd_mx4_logits_workspace_bytes(T, V, d):
 
 def fopd_mx4_logits(hidden, dt_hidden, ldh, weight, T, V, d, logits, dt, ld, workspace, stream=None):
     """weight: the packed [V, d] projection that fopd_mx4_quantize wrote."""
-    import torch
-    kinds = (torch.float32, torch.bfloat16)
-    wp, wn = _ws(weight)
+    wp, wn = _packed(weight, "weight")
     p, n = _ws(workspace)
-    _check(load_library().fopd_mx4_logits(_ptr(hidden, kinds, "hidden"), int(dt_hidden), int(ldh), wp, wn, int(T), int(V),
-                                          int(d), _ptr(logits, kinds, "logits"), int(dt), int(ld), p, n, _stream(stream)),
+    _check(load_library().fopd_mx4_logits(_matrix(hidden, dt_hidden, "hidden"), int(dt_hidden), int(ldh), wp, wn, int(T), int(V),
+                                          int(d), _matrix(logits, dt, "logits"), int(dt), int(ld), p, n, _stream(stream)),
            "fopd_mx4_logits")
 
 
@@ -609,10 +624,10 @@ def fopd_verify_draft(target_logits, draft_logits, dt, R, V, ld, ld_draft, draft
                       temperature, accept_u, noise, ld_noise, n_accepted, out_ids, out_logp, out_mask, workspace,
                       stream=None):
     import torch
-    kinds, f32, i32 = (torch.float32, torch.bfloat16), torch.float32, torch.int32
+    f32, i32 = torch.float32, torch.int32
     p, n = _ws(workspace)
     st = load_library().fopd_verify_draft(
-        _ptr(target_logits, kinds, "target_logits"), _ptr(draft_logits, kinds, "draft_logits"), int(dt), int(R), int(V),
+        _matrix(target_logits, dt, "target_logits"), _matrix(draft_logits, dt, "draft_logits"), int(dt), int(R), int(V),
         int(ld), int(ld_draft), _ptr(draft_ids, i32, "draft_ids"), _ptr(row_begin, torch.int64, "row_begin"),
         _ptr(draft_lens, i32, "draft_lens"), int(B), int(max_draft), _ptr(temperature, f32, "temperature"),
         _ptr(accept_u, f32, "accept_u"), _ptr(noise, f32, "noise"), int(ld_noise), _ptr(n_accepted, i32, "n_accepted"),

@@ -188,3 +188,51 @@ def test_gradient_list_refuses_what_it_cannot_describe():
             fb.grad_tensors(grads, outs)
     with pytest.raises(ValueError):
         fb.grad_tensors([torch.zeros(4)], [])
+
+
+class _OnDevice:
+    """What the binding looks at of a tensor."""
+    is_cuda = True
+
+    def __init__(self, dtype, contiguous=True):
+        self.dtype, self.contiguous = dtype, contiguous
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return 4096
+
+    def numel(self):
+        return 1 << 20
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+
+def test_matrices_of_another_type_than_named_and_packed_ones_elsewhere_are_refused():
+    """Read as the wider type a matrix would be run past; a packed weight in host memory is no address for the device."""
+    f32, bf16, host = _OnDevice(torch.float32), _OnDevice(torch.bfloat16), torch.zeros(1 << 16, dtype=torch.uint8)
+    packed, ws = _OnDevice(torch.uint8), (4096, 1 << 20)
+
+    def verify(target, draft, dt):
+        fb.fopd_verify_draft(target, draft, dt, 8, 64, 64, 64, 4096, None, None, 2, 3, None, 4096, 4096, 64, 4096, 4096, 4096, 4096, ws, stream=0)
+
+    def logits(h, dth, w, z, dt):
+        fb.fopd_mx4_logits(h, dth, 64, w, 8, 100, 64, z, dt, 104, ws, stream=0)
+
+    for call in (lambda: verify(f32, bf16, fb.FOPD_F32), lambda: verify(f32, bf16, fb.FOPD_BF16), lambda: verify(bf16, None, fb.FOPD_F32),
+                 lambda: fb.fopd_mx4_quantize(bf16, fb.FOPD_F32, 8, 64, 64, packed, stream=0),
+                 lambda: fb.fopd_mx4_quantize(bf16, fb.FOPD_BF16, 8, 64, 64, host, stream=0),
+                 lambda: fb.fopd_mx4_quantize(bf16, fb.FOPD_BF16, 8, 64, 64, _OnDevice(torch.uint8, False), stream=0),
+                 lambda: fb.fopd_mx4_dequantize(packed, 8, 64, bf16, fb.FOPD_F32, 64, stream=0),
+                 lambda: fb.fopd_mx4_dequantize(host, 8, 64, bf16, fb.FOPD_BF16, 64, stream=0),
+                 lambda: logits(bf16, fb.FOPD_F32, packed, f32, fb.FOPD_F32), lambda: logits(bf16, fb.FOPD_BF16, packed, bf16, fb.FOPD_F32),
+                 lambda: logits(bf16, fb.FOPD_BF16, host, f32, fb.FOPD_F32)):
+        with pytest.raises(ValueError):
+            call()
+    # the library's own refusals are still reached: a type that does not exist, a missing matrix
+    for call, status in ((lambda: verify(f32, f32, 5), 4), (lambda: verify(None, None, fb.FOPD_F32), 1)):
+        with pytest.raises(fb.FopdError) as refused:
+            call()
+        assert refused.value.status == status
