@@ -698,7 +698,8 @@ fopd_status fopd_verify_draft(const void* target_logits, const void* draft_logit
  *                  A norm that is NaN or infinite makes c NaN or 0, and the results accordingly.
  * A tensor is `rows` rows of `cols` entries, row r at grad + r ld; out likewise with ld_out, of the same shape.  Only the alignment of
  * the element type is needed (16 bytes are faster).  out == grad (then of the same type and pitch) clips in place; else
- * no memory may be shared.  A tensor has at most 2^40 entries; rows or cols of 0 are allowed, and so is n = 0 (sum 0).  fopd_grad_norm does not use out.
+ * no memory may be shared, nor between two tensors of a list that is clipped: a gradient that is listed twice would be scaled
+ * twice (fopd_grad_norm counts it twice).  A tensor has at most 2^40 entries; rows or cols of 0 are allowed, and so is n = 0 (sum 0).  fopd_grad_norm does not use out.
  * `tensors_host` is HOST memory, read before the call returns; the pointers in it are device pointers.
  *   workspace of fopd_grad_norm: fopd_grad_workspace_bytes() bytes, 256-byte aligned, initialised once with fopd_workspace_init
  */

@@ -40,8 +40,7 @@ constexpr int kGemmThreads = kLmThreads;
 // item takes 1.6 a step of 64 (with all compute units at work; 1.2 with sixteen) plus 13 for its first loads and its stores,
 // and the partial results are read at 4.5 TB/s when they are summed.  151,936 x 4096, the contraction alone, us by number of
 // runs: 256 rows 1: 2728, 8: 420, 16: 265; 512 rows 1: 2882, 4: 905, 8: 474, 16: 477; 768 rows 1: 3022, 4: 902, 8: 834, 16: 846
-// (5, which 240 items on 256 compute units seem to ask for: 1289); 2048 rows 1: 3637, 2: 1863, 4: 1871; 3072 rows 1: 3602, 4:
-// 2838, 8: 2887.
+// (5, which 240 items on 256 compute units seem to ask for: 1289); 2048 rows 1: 3637, 2: 1863, 4: 1871.
 inline int gemm_splits(int64_t M, int64_t N, int64_t K, int64_t most) {
   const int tiles_m = static_cast<int>((M + kGemmTile - 1) / kGemmTile);
   const int tiles_n = static_cast<int>((N + kGemmTile - 1) / kGemmTile);
