@@ -622,7 +622,8 @@ fopd_status fopd_lm_head_loss_fwd_bwd_topk_teacher(
  *   workspace          fopd_mx4_logits_workspace_bytes(T, V, d) bytes, 256-byte aligned; nothing in it has to be initialised
  * The sum over k of a result is taken in an order that goes by T, V and d, not by its place: the same hidden row in a call of
  * another T may differ in its last bits.  The first call in a process and on a device (with T > 0) sets kernel attributes: make
- * one call, of any size, before capturing fopd_mx4_logits into a HIP graph.  T = 0 or R = 0 does nothing.  Outputs share no memory with inputs.
+ * one call, of any size, before capturing fopd_mx4_logits into a HIP graph.  T = 0 or R = 0 does nothing and needs no buffers.
+ * Outputs share no memory with inputs.
  */
 size_t fopd_mx4_bytes(int64_t R, int64_t d);
 fopd_status fopd_mx4_quantize(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed,

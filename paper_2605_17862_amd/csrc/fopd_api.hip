@@ -184,9 +184,14 @@ inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintp
 // Of a row: the kernels form the places behind its last vector, one a lane, in 32 bits, up to 512 lanes of them.
 constexpr int64_t kMaxColumns = (1LL << 31) - 512;
 
-fopd_status check_matrix(const void* m, fopd_dtype dt, int64_t T, int64_t V, int64_t ld) {
+fopd_status check_shape(fopd_dtype dt, int64_t T, int64_t V, int64_t ld) {
   if (dt != FOPD_F32 && dt != FOPD_BF16) return FOPD_EDTYPE;
-  if (T < 0 || T > 2147483647LL || V <= 0 || ld < V || V > kMaxColumns) return FOPD_ESHAPE;
+  return T < 0 || T > 2147483647LL || V <= 0 || ld < V || V > kMaxColumns ? FOPD_ESHAPE : FOPD_OK;
+}
+
+fopd_status check_matrix(const void* m, fopd_dtype dt, int64_t T, int64_t V, int64_t ld) {
+  const fopd_status st = check_shape(dt, T, V, ld);
+  if (st != FOPD_OK) return st;
   if (m == nullptr) return FOPD_EINVAL;
   const size_t es = (dt == FOPD_F32) ? 4 : 2;
   if (misaligned(m, 16) || (static_cast<size_t>(ld) * es) % 16 != 0) return FOPD_EALIGN;
@@ -663,6 +668,12 @@ fopd_status check_mx4(const void* packed, size_t bytes, int64_t R, int64_t d) {
   if (misaligned(packed, 16)) return FOPD_EALIGN;
   if (bytes < static_cast<size_t>(Mx4Layout(R, d).total)) return FOPD_EWORKSPACE;
   return FOPD_OK;
+}
+
+// Of a call without rows, whose buffers may be empty: no addresses.
+fopd_status check_no_rows(fopd_dtype dt, int64_t d, int64_t ld) {
+  const fopd_status st = check_shape(dt, 0, d, ld);
+  return st == FOPD_OK && d > kMxMaxEntries ? FOPD_ESHAPE : st;
 }
 
 // launch(first group of 64 rows, workgroups): one for each group and step.
@@ -2059,19 +2070,21 @@ size_t fopd_mx4_bytes(int64_t R, int64_t d) {
 
 fopd_status fopd_mx4_quantize(const void* in, fopd_dtype dt, int64_t R, int64_t d, int64_t ld, void* packed,
                               size_t packed_bytes, void* stream) {
+  if (R == 0) return check_no_rows(dt, d, ld);
   fopd_status st = check_matrix(in, dt, R, d, ld);
   if (st != FOPD_OK) return st;
   st = check_mx4(packed, packed_bytes, R, d);
-  if (st != FOPD_OK || R == 0) return st;
+  if (st != FOPD_OK) return st;
   return launch_mx4_pack(in, dt, R, d, ld, packed, static_cast<hipStream_t>(stream));
 }
 
 fopd_status fopd_mx4_dequantize(const void* packed, size_t packed_bytes, int64_t R, int64_t d, void* out, fopd_dtype dt,
                                 int64_t ldo, void* stream) {
+  if (R == 0) return check_no_rows(dt, d, ldo);
   fopd_status st = check_matrix(out, dt, R, d, ldo);
   if (st != FOPD_OK) return st;
   st = check_mx4(packed, packed_bytes, R, d);
-  if (st != FOPD_OK || R == 0) return st;
+  if (st != FOPD_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto kern = dt == FOPD_BF16 ? fopd_mx4_unpack<FOPD_BF16> : fopd_mx4_unpack<FOPD_F32>;
   return mx4_in_slabs(Mx4Layout(R, d), [&](int64_t g, unsigned n) {
@@ -2087,16 +2100,16 @@ size_t fopd_mx4_logits_workspace_bytes(int64_t T, int64_t V, int64_t d) {
 fopd_status fopd_mx4_logits(const void* hidden, fopd_dtype dt_hidden, int64_t ldh, const void* weight, size_t weight_bytes,
                             int64_t T, int64_t V, int64_t d, void* logits, fopd_dtype dt, int64_t ld, void* workspace,
                             size_t workspace_bytes, void* stream) {
-  fopd_status st = check_matrix(hidden, dt_hidden, T, d, ldh);
+  fopd_status st = T == 0 ? check_no_rows(dt_hidden, d, ldh) : check_matrix(hidden, dt_hidden, T, d, ldh);
   if (st != FOPD_OK) return st;
-  st = check_matrix(logits, dt, T, V, ld);
-  if (st != FOPD_OK) return st;
-  st = check_mx4(weight, weight_bytes, V, d);
+  st = T == 0 ? check_shape(dt, T, V, ld) : check_matrix(logits, dt, T, V, ld);
   if (st != FOPD_OK) return st;
   if (V > kMxMaxVocabulary) return FOPD_ESHAPE;
+  if (T == 0) return FOPD_OK;
+  st = check_mx4(weight, weight_bytes, V, d);
+  if (st != FOPD_OK) return st;
   if (workspace == nullptr || misaligned(workspace, 256) || workspace_bytes < fopd_mx4_logits_workspace_bytes(T, V, d))
     return FOPD_EWORKSPACE;
-  if (T == 0) return FOPD_OK;
   if ((st = allow_mx4_tiles()) != FOPD_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (mx4_raw_rows(T, V)) return launch_mx4_raw(static_cast<const unsigned char*>(weight), V, hidden, dt_hidden, ldh, T, d, logits, dt, ld, s);

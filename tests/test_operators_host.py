@@ -67,6 +67,31 @@ def test_mx4_rejects_bad_arguments_before_launch():
     assert logits(T=0) == 0
 
 
+def test_mx4_calls_without_rows_need_no_buffers():
+    """Empty tensors have no address; sizes and types are looked at all the same."""
+    lib = fb.load_library()
+
+    def quantize(dt=1, d=64, ld=64):
+        return lib.fopd_mx4_quantize(None, dt, 0, d, ld, None, 0, None)
+
+    def dequantize(dt=1, d=64, ld=64):
+        return lib.fopd_mx4_dequantize(None, 0, 0, d, None, dt, ld, None)
+
+    def logits(dt=1, d=64, ld=64, dtz=0, V=100, ldz=100, w=8192, wn=1 << 20):
+        return lib.fopd_mx4_logits(None, dt, ld, P(w), wn, 0, V, d, None, dtz, ldz, None, 0, None)
+
+    for call in (quantize, dequantize, logits):
+        assert call() == 0
+        assert call(dt=2) == 4
+        assert call(d=0) == 2
+        assert call(ld=63) == 2
+        assert call(d=(1 << 24) + 8, ld=1 << 25) == 2
+    assert logits(dtz=7) == 4
+    assert logits(V=0) == 2
+    assert logits(ldz=99) == 2
+    assert logits(V=(1 << 28) + 64, ldz=1 << 29) == 2
+
+
 def _verify(lib, **kw):
     a = dict(z=4096, zd=8192, dt=1, R=8, V=64, ld=64, ldd=64, ids=4096, row=None, lens=None, B=2, K=3, tau=None, u=4096, e=4096,
              lde=64, n=4096, oi=4096, ol=4096, om=4096, ws=4096, wsn=1 << 22)
